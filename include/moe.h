@@ -37,6 +37,9 @@ typedef enum moe_status {
   MOE_ERR_ARCH = -6               /* the current device is not sm_100 */
 } moe_status;
 
+/* Element types of the operators that take more than bf16. */
+typedef enum moe_dtype { MOE_BF16 = 0, MOE_FP16 = 1, MOE_FP32 = 2 } moe_dtype;
+
 #define MOE_MAX_EXPERTS 16
 
 typedef struct moe_layer moe_layer_t; /* opaque, owned by the library */
@@ -270,6 +273,51 @@ long moe_num_subsets(int E, int r);
  * x, out [T][h] bf16 device (may alias); stream is a cudaStream_t.
  */
 int moe_rmsnorm(const void* x, int T, int h, float eps, void* out, void* cuda_stream);
+
+/*
+ * Residual addition with RMS norm, what a pre-norm block computes between two layers:
+ *   s = x + residual, rounded to the tensors' type (the residual stream holds it),
+ *   out = s * rstd * gain,  rstd = 1 / sqrt(mean(s^2) + eps),
+ * everything between load and store in fp32; the norm is of s as it is held.
+ *   x, residual, out, s [T][h], gain [h]  device, dtype (a moe_dtype); any h in
+ *   1 .. 2^20.  residual NULL: s = x and the argument s is NULL too.  gain NULL: 1.
+ *   rstd [T] fp32 device, or NULL: what the backward pass wants.
+ * out and s may each be x or residual themselves (the same address); no other
+ * overlap is allowed.  T = 0 is a no-op.  Asynchronous.
+ */
+int moe_add_rmsnorm(const void* x, const void* residual, const void* gain, int T, int h, float eps,
+                    int dtype, void* out, void* s, float* rstd, void* cuda_stream);
+
+/*
+ * The same norm with an output in 8 bits: v = s * rstd * gain in fp32,
+ *   scale = max(max |v| / 448, 2^-126) over a row (group = 0) or over each 128
+ *   columns of it (group = 128, h % 128 == 0),  q = e4m3(v / scale), to nearest even.
+ *   q [T][h] e4m3 device (its value times its scale is v),
+ *   scales [T] or [T][h / 128] fp32 device.
+ * A NaN of v is a NaN of q and counts in no maximum.  q may not overlap an input.
+ */
+int moe_add_rmsnorm_e4m3(const void* x, const void* residual, const void* gain, int T, int h,
+                         float eps, int dtype, int group, void* q, float* scales, void* s,
+                         void* cuda_stream);
+
+/*
+ * Gradients of moe_add_rmsnorm, from its s and rstd.  With hat = s * rstd and
+ * g = d_out * gain:
+ *   dx = d_s + rstd * (g - hat * mean(g * hat))    the gradient of x and of residual alike,
+ *   dgain = sum over the rows of d_out * hat.
+ *   d_out, d_s, s, dx [T][h], gain, dgain [h] device, dtype.  d_s: the gradient that
+ *   reaches s on its own way (the residual stream), or NULL for 0; dx may be d_s
+ *   itself, no other overlap is allowed.  gain NULL: 1.  dgain NULL: not computed.
+ *   workspace: device memory of moe_add_rmsnorm_backward_workspace(T, h) bytes for
+ *   the current device (needed with dgain only), free again when the call's
+ *   kernels are done.
+ * The sums have a fixed order: the same call gives the same bits.  T = 0 clears
+ * dgain.  Asynchronous.
+ */
+int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, const float* rstd,
+                             const void* gain, int T, int h, int dtype, void* dx, void* dgain,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t moe_add_rmsnorm_backward_workspace(int T, int h);
 
 /*
  * A stack of MoE layers with attention left out:

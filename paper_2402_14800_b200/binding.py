@@ -70,6 +70,11 @@ def load_library(path: str | None = None):
     lib.moe_num_subsets.restype = ctypes.c_long
     lib.moe_num_subsets.argtypes = [ci, ci]
     lib.moe_rmsnorm.argtypes = [vp, ci, ci, cf, vp, vp]
+    lib.moe_add_rmsnorm.argtypes = [vp, vp, vp, ci, ci, cf, ci, vp, vp, vp, vp]
+    lib.moe_add_rmsnorm_e4m3.argtypes = [vp, vp, vp, ci, ci, cf, ci, ci, vp, vp, vp, vp]
+    lib.moe_add_rmsnorm_backward_workspace.restype = ctypes.c_size_t
+    lib.moe_add_rmsnorm_backward_workspace.argtypes = [ci, ci]
+    lib.moe_add_rmsnorm_backward.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, ctypes.c_size_t, vp]
     lib.moe_stack_forward.argtypes = [ctypes.POINTER(vp), ci, vp, ci, ctypes.POINTER(cf), cf, vp]
     lib.moe_coselection.argtypes = [vp, vp, ci, ctypes.POINTER(ctypes.c_int32)]
     lib.moe_frequency_subset.restype = u32
@@ -338,6 +343,129 @@ def rmsnorm(x, eps: float = 1e-5, out=None, stream=None):
     st = stream or torch.cuda.current_stream(x.device)
     _check(load_library().moe_rmsnorm(x.data_ptr(), T, h, eps, out.data_ptr(), ctypes.c_void_p(st.cuda_stream)))
     return out
+
+
+# Operators on the caller's own tensors: no handle, scratch from torch's allocator on the call's stream.
+
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _operand(name, t, dtype, shape, device) -> int:
+    """Address of a contiguous tensor of this type, shape and device; 0 for None."""
+    if t is None:
+        return 0
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or tuple(t.shape) != shape \
+            or not t.is_contiguous():
+        raise MoeError(-1, "%s must be a contiguous %s tensor of shape %s on %s, got %s" % (
+            name, dtype, shape, device,
+            "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride()) if isinstance(t, torch.Tensor)
+            else type(t).__name__))
+    return t.data_ptr()
+
+
+class _Call:
+    """The device and stream of one call: the tensors' device is current inside it, and memory that it takes
+    from torch's allocator belongs to the stream that it launches on."""
+
+    def __init__(self, x, dims, stream):
+        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == dims and x.dtype in DTYPES):
+            raise MoeError(-1, "expected a %d-dimensional CUDA tensor of bf16, fp16 or fp32" % dims)
+        self.device, self.dtype, self.code = x.device, x.dtype, DTYPES[x.dtype]
+        if stream is not None and stream.device != x.device:
+            raise MoeError(-1, "the stream is on %s, the tensors on %s" % (stream.device, x.device))
+        current = torch.cuda.current_device() == x.device.index
+        self.stream = stream
+        if stream is not None:
+            self.guard = torch.cuda.stream(stream)  # makes the stream's device current too
+        else:
+            self.guard = None if current else torch.cuda.device(x.device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        st = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
+        self.handle = st.cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def empty(self, shape, dtype=None):
+        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+
+
+def add_rmsnorm(x, residual=None, gain=None, eps: float = 1e-5, out=None, s=None, rstd=None, stream=None):
+    """``moe_add_rmsnorm``: s = x + residual (in their type), out = s / sqrt(mean(s^2) + eps) * gain.
+
+    x, residual, out, s [T, h] bf16, fp16 or fp32, gain [h] of the same type (None: 1).  Without a residual
+    s is x.  ``rstd``: an fp32 tensor [T] that receives 1 / sqrt(...) for the backward pass.
+    Returns (out, s)."""
+    with _Call(x, 2, stream) as c:
+        T, h = shape = tuple(x.shape)
+        if residual is None:
+            if s is not None:
+                raise MoeError(-1, "without a residual s is x itself")
+        elif s is None:
+            s = c.empty(shape)
+        if out is None:
+            out = c.empty(shape)
+        _check(load_library().moe_add_rmsnorm(
+            _operand("x", x, c.dtype, shape, c.device), _operand("residual", residual, c.dtype, shape, c.device),
+            _operand("gain", gain, c.dtype, (h,), c.device), T, h, eps, c.code,
+            _operand("out", out, c.dtype, shape, c.device), _operand("s", s, c.dtype, shape, c.device),
+            _operand("rstd", rstd, torch.float32, (T,), c.device), c.handle))
+        return out, x if residual is None else s
+
+
+def add_rmsnorm_e4m3(x, residual=None, gain=None, eps: float = 1e-5, group: int = 0, q=None, scales=None, s=None,
+                     stream=None):
+    """``moe_add_rmsnorm_e4m3``: the norm of ``add_rmsnorm`` in 8 bits.  q [T, h] float8_e4m3fn and fp32
+    ``scales``, one a row ([T, 1], group 0) or one for each 128 columns ([T, h / 128], group 128);
+    q * scales is the normalised value.  Returns (q, scales, s)."""
+    with _Call(x, 2, stream) as c:
+        T, h = shape = tuple(x.shape)
+        if residual is None:
+            if s is not None:
+                raise MoeError(-1, "without a residual s is x itself")
+        elif s is None:
+            s = c.empty(shape)
+        if q is None:
+            q = c.empty(shape, torch.float8_e4m3fn)
+        n = h // group if group > 0 else 1
+        if scales is None:
+            scales = c.empty((T, n), torch.float32)
+        _check(load_library().moe_add_rmsnorm_e4m3(
+            _operand("x", x, c.dtype, shape, c.device), _operand("residual", residual, c.dtype, shape, c.device),
+            _operand("gain", gain, c.dtype, (h,), c.device), T, h, eps, c.code, group,
+            _operand("q", q, torch.float8_e4m3fn, shape, c.device),
+            _operand("scales", scales, torch.float32, (T, n), c.device),
+            _operand("s", s, c.dtype, shape, c.device), c.handle))
+        return q, scales, x if residual is None else s
+
+
+def add_rmsnorm_backward(d_out, s, rstd, gain=None, d_s=None, dx=None, dgain=None, stream=None):
+    """``moe_add_rmsnorm_backward``: gradients of ``add_rmsnorm`` from its s and rstd.  ``d_s``: the gradient
+    that reaches s along the residual stream (None: 0).  Returns (dx, dgain): dx belongs to x and to the
+    residual alike; dgain is None without a gain."""
+    with _Call(d_out, 2, stream) as c:
+        T, h = shape = tuple(d_out.shape)
+        if dx is None:
+            dx = c.empty(shape)
+        if gain is not None and dgain is None:
+            dgain = c.empty((h,))
+        lib = load_library()
+        ws, n = None, 0
+        if dgain is not None:
+            n = lib.moe_add_rmsnorm_backward_workspace(T, h)
+            ws = c.empty((n,), torch.uint8)
+        _check(lib.moe_add_rmsnorm_backward(
+            _operand("d_out", d_out, c.dtype, shape, c.device), _operand("d_s", d_s, c.dtype, shape, c.device),
+            _operand("s", s, c.dtype, shape, c.device), _operand("rstd", rstd, torch.float32, (T,), c.device),
+            _operand("gain", gain, c.dtype, (h,), c.device), T, h, c.code,
+            _operand("dx", dx, c.dtype, shape, c.device), _operand("dgain", dgain, c.dtype, (h,), c.device),
+            ws.data_ptr() if ws is not None else None, n, c.handle))
+        return dx, dgain
 
 
 def stack_forward(layers, x, betas=None, eps: float = 1e-5, y=None):
