@@ -350,49 +350,49 @@ def rmsnorm(x, eps: float = 1e-5, out=None, stream=None):
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-def _operand(name, t, dtype, shape, device) -> int:
-    """Address of a contiguous tensor of this type, shape and device; 0 for None."""
+_raw_stream = torch._C._cuda_getCurrentRawStream  # a tenth of the time of torch.cuda.current_stream().cuda_stream
+
+
+def _operand(name, t, dtype, shape, index):
+    """Address of a contiguous tensor of this type and shape on this device; None for None."""
     if t is None:
-        return 0
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device or tuple(t.shape) != shape \
-            or not t.is_contiguous():
-        raise MoeError(-1, "%s must be a contiguous %s tensor of shape %s on %s, got %s" % (
-            name, dtype, shape, device,
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index
+            and t.is_contiguous()):
+        raise MoeError(-1, "%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s" % (
+            name, dtype, tuple(shape), index,
             "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride()) if isinstance(t, torch.Tensor)
             else type(t).__name__))
     return t.data_ptr()
 
 
-class _Call:
-    """The device and stream of one call: the tensors' device is current inside it, and memory that it takes
-    from torch's allocator belongs to the stream that it launches on."""
+def _on_device_of(x, dims, stream, body, *args):
+    """body(device index, stream handle, *args) with the device of ``x`` current; memory that it takes from torch's
+    allocator belongs to the stream that it launches on."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == dims and x.dtype in DTYPES):
+        raise MoeError(-1, "expected a %d-dimensional CUDA tensor of bf16, fp16 or fp32" % dims)
+    index = x.get_device()
+    if stream is not None:
+        if stream.device_index != index:
+            raise MoeError(-1, "the stream is on cuda:%d, the tensors on cuda:%d" % (stream.device_index, index))
+        with torch.cuda.stream(stream):  # makes the stream's device current too
+            return body(index, stream.cuda_stream, *args)
+    if torch.cuda.current_device() == index:
+        return body(index, _raw_stream(index), *args)
+    with torch.cuda.device(index):
+        return body(index, _raw_stream(index), *args)
 
-    def __init__(self, x, dims, stream):
-        if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == dims and x.dtype in DTYPES):
-            raise MoeError(-1, "expected a %d-dimensional CUDA tensor of bf16, fp16 or fp32" % dims)
-        self.device, self.dtype, self.code = x.device, x.dtype, DTYPES[x.dtype]
-        if stream is not None and stream.device != x.device:
-            raise MoeError(-1, "the stream is on %s, the tensors on %s" % (stream.device, x.device))
-        current = torch.cuda.current_device() == x.device.index
-        self.stream = stream
-        if stream is not None:
-            self.guard = torch.cuda.stream(stream)  # makes the stream's device current too
-        else:
-            self.guard = None if current else torch.cuda.device(x.device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        st = self.stream if self.stream is not None else torch.cuda.current_stream(self.device)
-        self.handle = st.cuda_stream
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-    def empty(self, shape, dtype=None):
-        return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
+def _sum_buffer(x, residual, s, index):
+    """Address of s (a new tensor where the caller gave none), and s itself."""
+    if residual is None:
+        if s is not None:
+            raise MoeError(-1, "without a residual s is x itself")
+        return None, x
+    if s is None:
+        s = torch.empty_like(x)
+        return s.data_ptr(), s
+    return _operand("s", s, x.dtype, x.shape, index), s
 
 
 def add_rmsnorm(x, residual=None, gain=None, eps: float = 1e-5, out=None, s=None, rstd=None, stream=None):
@@ -401,21 +401,20 @@ def add_rmsnorm(x, residual=None, gain=None, eps: float = 1e-5, out=None, s=None
     x, residual, out, s [T, h] bf16, fp16 or fp32, gain [h] of the same type (None: 1).  Without a residual
     s is x.  ``rstd``: an fp32 tensor [T] that receives 1 / sqrt(...) for the backward pass.
     Returns (out, s)."""
-    with _Call(x, 2, stream) as c:
-        T, h = shape = tuple(x.shape)
-        if residual is None:
-            if s is not None:
-                raise MoeError(-1, "without a residual s is x itself")
-        elif s is None:
-            s = c.empty(shape)
-        if out is None:
-            out = c.empty(shape)
-        _check(load_library().moe_add_rmsnorm(
-            _operand("x", x, c.dtype, shape, c.device), _operand("residual", residual, c.dtype, shape, c.device),
-            _operand("gain", gain, c.dtype, (h,), c.device), T, h, eps, c.code,
-            _operand("out", out, c.dtype, shape, c.device), _operand("s", s, c.dtype, shape, c.device),
-            _operand("rstd", rstd, torch.float32, (T,), c.device), c.handle))
-        return out, x if residual is None else s
+    return _on_device_of(x, 2, stream, _add_rmsnorm, x, residual, gain, eps, out, s, rstd)
+
+
+def _add_rmsnorm(index, st, x, residual, gain, eps, out, s, rstd):
+    T, h = shape = x.shape
+    dt = x.dtype
+    xp, rp = _operand("x", x, dt, shape, index), _operand("residual", residual, dt, shape, index)
+    gp, tp = _operand("gain", gain, dt, (h,), index), _operand("rstd", rstd, torch.float32, (T,), index)
+    sp, s = _sum_buffer(x, residual, s, index)
+    if out is None:
+        out = torch.empty_like(x)
+    op = _operand("out", out, dt, shape, index)
+    _check(load_library().moe_add_rmsnorm(xp, rp, gp, T, h, eps, DTYPES[dt], op, sp, tp, st))
+    return out, s
 
 
 def add_rmsnorm_e4m3(x, residual=None, gain=None, eps: float = 1e-5, group: int = 0, q=None, scales=None, s=None,
@@ -423,49 +422,53 @@ def add_rmsnorm_e4m3(x, residual=None, gain=None, eps: float = 1e-5, group: int 
     """``moe_add_rmsnorm_e4m3``: the norm of ``add_rmsnorm`` in 8 bits.  q [T, h] float8_e4m3fn and fp32
     ``scales``, one a row ([T, 1], group 0) or one for each 128 columns ([T, h / 128], group 128);
     q * scales is the normalised value.  Returns (q, scales, s)."""
-    with _Call(x, 2, stream) as c:
-        T, h = shape = tuple(x.shape)
-        if residual is None:
-            if s is not None:
-                raise MoeError(-1, "without a residual s is x itself")
-        elif s is None:
-            s = c.empty(shape)
-        if q is None:
-            q = c.empty(shape, torch.float8_e4m3fn)
-        n = h // group if group > 0 else 1
-        if scales is None:
-            scales = c.empty((T, n), torch.float32)
-        _check(load_library().moe_add_rmsnorm_e4m3(
-            _operand("x", x, c.dtype, shape, c.device), _operand("residual", residual, c.dtype, shape, c.device),
-            _operand("gain", gain, c.dtype, (h,), c.device), T, h, eps, c.code, group,
-            _operand("q", q, torch.float8_e4m3fn, shape, c.device),
-            _operand("scales", scales, torch.float32, (T, n), c.device),
-            _operand("s", s, c.dtype, shape, c.device), c.handle))
-        return q, scales, x if residual is None else s
+    return _on_device_of(x, 2, stream, _add_rmsnorm_e4m3, x, residual, gain, eps, group, q, scales, s)
+
+
+def _add_rmsnorm_e4m3(index, st, x, residual, gain, eps, group, q, scales, s):
+    T, h = shape = x.shape
+    dt = x.dtype
+    xp, rp = _operand("x", x, dt, shape, index), _operand("residual", residual, dt, shape, index)
+    gp = _operand("gain", gain, dt, (h,), index)
+    sp, s = _sum_buffer(x, residual, s, index)
+    if q is None:
+        q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+    qp = _operand("q", q, torch.float8_e4m3fn, shape, index)
+    n = h // group if group > 0 else 1
+    if scales is None:
+        scales = x.new_empty((T, n), dtype=torch.float32)
+    cp = _operand("scales", scales, torch.float32, (T, n), index)
+    _check(load_library().moe_add_rmsnorm_e4m3(xp, rp, gp, T, h, eps, DTYPES[dt], group, qp, cp, sp, st))
+    return q, scales, s
 
 
 def add_rmsnorm_backward(d_out, s, rstd, gain=None, d_s=None, dx=None, dgain=None, stream=None):
     """``moe_add_rmsnorm_backward``: gradients of ``add_rmsnorm`` from its s and rstd.  ``d_s``: the gradient
     that reaches s along the residual stream (None: 0).  Returns (dx, dgain): dx belongs to x and to the
     residual alike; dgain is None without a gain."""
-    with _Call(d_out, 2, stream) as c:
-        T, h = shape = tuple(d_out.shape)
-        if dx is None:
-            dx = c.empty(shape)
-        if gain is not None and dgain is None:
-            dgain = c.empty((h,))
-        lib = load_library()
-        ws, n = None, 0
-        if dgain is not None:
-            n = lib.moe_add_rmsnorm_backward_workspace(T, h)
-            ws = c.empty((n,), torch.uint8)
-        _check(lib.moe_add_rmsnorm_backward(
-            _operand("d_out", d_out, c.dtype, shape, c.device), _operand("d_s", d_s, c.dtype, shape, c.device),
-            _operand("s", s, c.dtype, shape, c.device), _operand("rstd", rstd, torch.float32, (T,), c.device),
-            _operand("gain", gain, c.dtype, (h,), c.device), T, h, c.code,
-            _operand("dx", dx, c.dtype, shape, c.device), _operand("dgain", dgain, c.dtype, (h,), c.device),
-            ws.data_ptr() if ws is not None else None, n, c.handle))
-        return dx, dgain
+    return _on_device_of(d_out, 2, stream, _add_rmsnorm_backward, d_out, s, rstd, gain, d_s, dx, dgain)
+
+
+def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
+    T, h = shape = d_out.shape
+    dt = d_out.dtype
+    dp, sp = _operand("d_out", d_out, dt, shape, index), _operand("s", s, dt, shape, index)
+    ep, gp = _operand("d_s", d_s, dt, shape, index), _operand("gain", gain, dt, (h,), index)
+    tp = _operand("rstd", rstd, torch.float32, (T,), index)
+    if dx is None:
+        dx = torch.empty_like(d_out)
+    xp = _operand("dx", dx, dt, shape, index)
+    if gain is not None and dgain is None:
+        dgain = torch.empty_like(gain)
+    lib = load_library()
+    wp, n = None, 0
+    if dgain is not None:
+        n = lib.moe_add_rmsnorm_backward_workspace(T, h)
+        ws = d_out.new_empty((n,), dtype=torch.uint8)
+        wp = ws.data_ptr()
+    _check(lib.moe_add_rmsnorm_backward(dp, ep, sp, tp, gp, T, h, DTYPES[dt], xp,
+                                        _operand("dgain", dgain, dt, (h,), index), wp, n, st))
+    return dx, dgain
 
 
 def stack_forward(layers, x, betas=None, eps: float = 1e-5, y=None):

@@ -98,19 +98,26 @@ template <int E> __device__ __forceinline__ float group_max(float v) {
   return v;
 }
 
-template <typename T, int E>
-__device__ __forceinline__ void store_e4m3(uint8_t* q, const float* v, float scale) {
-  if (E == 1) {
-    *q = (uint8_t)__nv_cvt_float_to_fp8(v[0] / scale, __NV_SATFINITE, __NV_E4M3);
-  } else {
-    uint32_t w[(E + 3) / 4] = {};
+// Scale of a group and the factor that takes p = s * gain to q.  rstd cancels in v / scale: with m = max |p| it is
+// p * (448 / m), two roundings where v / scale has five (of 16-bit types p is exact in fp32), and one division a
+// group.  Groups whose scale is at its lower limit, whose 448 / m is no number, or whose rstd is none (a NaN in the
+// row) take v / scale itself: factor 0.
+__device__ __forceinline__ float2 scale_of(float m, float rstd) {
+  const float scale = fmaxf(m * rstd / kE4m3Max, kMinScale), f = kE4m3Max / m;
+  return make_float2(scale, scale > kMinScale && f < 3.0e38f ? f : 0.f);
+}
+
+template <int E> __device__ __forceinline__ void store_e4m3(uint8_t* q, float* p, float2 sc, float rstd) {
 #pragma unroll
-    for (int i = 0; i < E; i += 2) {
-      const uint32_t p = __nv_cvt_float2_to_fp8x2(make_float2(v[i] / scale, v[i + 1 < E ? i + 1 : i] / scale),
-                                                  __NV_SATFINITE, __NV_E4M3);
-      w[i / 4] |= p << (8 * (i & 3));
-    }
-    if (E == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[(E + 3) / 4 - 1]);
+  for (int i = 0; i < E; ++i) p[i] = sc.y > 0.f ? p[i] * sc.y : p[i] * rstd / sc.x;
+  if constexpr (E == 1) {
+    *q = (uint8_t)__nv_cvt_float_to_fp8(p[0], __NV_SATFINITE, __NV_E4M3);
+  } else {
+    uint32_t w[E / 4] = {};
+#pragma unroll
+    for (int i = 0; i < E; i += 2)
+      w[i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(p[i], p[i + 1]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+    if constexpr (E == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(q) = w[0];
   }
 }
@@ -192,7 +199,7 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
           mx[i] = 0.f;
           if (live && i * TPR + lane < nvec) {
 #pragma unroll
-            for (int k = 0; k < E; ++k) mx[i] = fmaxf(mx[i], fabsf(s[i].get(k) * rstd * gain[i].get(k)));
+            for (int k = 0; k < E; ++k) mx[i] = fmaxf(mx[i], fabsf(s[i].get(k) * gain[i].get(k)));
           }
           if constexpr (E > 1) {
             if (a.group) mx[i] = group_max<E>(mx[i]);
@@ -208,15 +215,15 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
           if (!live || v >= nvec) continue;
           const size_t o = (size_t)row * h + (size_t)v * E;
           if (add) s[i].store(reinterpret_cast<T*>(a.s) + o);
-          const float scale = fmaxf((a.group ? mx[i] : all) / kE4m3Max, kMinScale);
-          float y[E];
+          const float2 sc = scale_of(a.group ? mx[i] : all, rstd);
+          float p[E];
 #pragma unroll
-          for (int k = 0; k < E; ++k) y[k] = s[i].get(k) * rstd * gain[i].get(k);
-          store_e4m3<T, E>(reinterpret_cast<uint8_t*>(a.out) + o, y, scale);
+          for (int k = 0; k < E; ++k) p[k] = s[i].get(k) * gain[i].get(k);
+          store_e4m3<E>(reinterpret_cast<uint8_t*>(a.out) + o, p, sc, rstd);
           if (a.group) {
-            if (v % (128 / E) == 0) a.scales[(size_t)row * (h / 128) + v / (128 / E)] = scale;
+            if (v % (128 / E) == 0) a.scales[(size_t)row * (h / 128) + v / (128 / E)] = sc.x;
           } else if (v == 0) {
-            a.scales[row] = scale;
+            a.scales[row] = sc.x;
           }
         }
       }
@@ -249,7 +256,7 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
         s.load(hp + (size_t)v * E);
         if (gp) g.load(gp + (size_t)v * E);
 #pragma unroll
-        for (int k = 0; k < E; ++k) y[k] = s.get(k) * rstd * (gp ? g.get(k) : 1.f);
+        for (int k = 0; k < E; ++k) y[k] = (Q ? s.get(k) : s.get(k) * rstd) * (gp ? g.get(k) : 1.f);
       };
       float all = 0.f;
       if (Q && !a.group) {
@@ -276,12 +283,12 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
         if (v >= nvec) continue;
         const size_t o = (size_t)row * h + (size_t)v * E;
         if (Q) {
-          const float scale = fmaxf((a.group ? mx : all) / kE4m3Max, kMinScale);
-          store_e4m3<T, E>(reinterpret_cast<uint8_t*>(a.out) + o, y, scale);
+          const float2 sc = scale_of(a.group ? mx : all, rstd);
+          store_e4m3<E>(reinterpret_cast<uint8_t*>(a.out) + o, y, sc, rstd);
           if (a.group) {
-            if (v % (128 / E) == 0) a.scales[(size_t)row * (h / 128) + v / (128 / E)] = scale;
+            if (v % (128 / E) == 0) a.scales[(size_t)row * (h / 128) + v / (128 / E)] = sc.x;
           } else if (v == 0) {
-            a.scales[row] = scale;
+            a.scales[row] = sc.x;
           }
         } else {
           V w;
@@ -350,16 +357,25 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_backward_ker
       }
     };
     int odd = 0;
+    fetch(row);
     for (int base = blockIdx.x * kRows; base < a.T; base += step, row += step, odd ^= 1) {
       const bool live = row < a.T;
-      fetch(row);
+      V d0[NV], s0[NV], e0[NV];
+      const float rstd0 = rstd;
       float c = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        d0[i] = d[i];
+        s0[i] = s[i];
+        if (ep) e0[i] = e[i];
+      }
+      fetch(row + step);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         if (!live || i * TPR + lane >= nvec) continue;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          const float dh = d[i].get(k) * (s[i].get(k) * rstd);
+          const float dh = d0[i].get(k) * (s0[i].get(k) * rstd0);
           acc[i][k] += dh;
           c = fmaf(dh, gain[i].get(k), c);
         }
@@ -372,8 +388,8 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_backward_ker
         V y;
 #pragma unroll
         for (int k = 0; k < E; ++k) {
-          const float g = d[i].get(k) * gain[i].get(k), hat = s[i].get(k) * rstd;
-          y.set(k, fmaf(rstd, g - hat * c, ep ? e[i].get(k) : 0.f));
+          const float g = d0[i].get(k) * gain[i].get(k), hat = s0[i].get(k) * rstd0;
+          y.set(k, fmaf(rstd0, g - hat * c, ep ? e0[i].get(k) : 0.f));
         }
         y.store(reinterpret_cast<T*>(a.dx) + (size_t)row * h + (size_t)v * E);
       }
