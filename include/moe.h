@@ -320,6 +320,50 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
 size_t moe_add_rmsnorm_backward_workspace(int T, int h);
 
 /*
+ * Dense gated feed-forward block on the caller's own weights: the dense layer of a
+ * model, or the expert that runs beside the routed ones.
+ *   g = x W1^T,  u = x W3^T,  a = silu(g) * u,  y = a W2^T [+ residual]
+ *   x, residual, y [T][h], W1, W3 [f][h], W2 [h][f] device, dtype MOE_BF16 or
+ *   MOE_FP16; h and f multiples of 8 in 8 .. 2^20.  residual NULL: 0; y may be the
+ *   residual itself, no other overlap is allowed.
+ *   saved: NULL, or device memory of moe_ffn_saved_bytes(T, f) bytes that receives
+ *   g and u in fp32 ([T][f][2]) for moe_ffn_backward.
+ *   workspace: device memory of moe_ffn_forward_workspace(T, h, f) bytes for the
+ *   current device, free again when the call's kernels are done; calls that may
+ *   run at the same time need one each.
+ * a is rounded to the tensors' type, y once; everything else is fp32.  Both
+ * projections, the activation and the product are one launch.  The weights are
+ * read where they are: nothing is kept between calls.  T = 0 is a no-op.
+ * Asynchronous, and free of host synchronisation and allocation.
+ */
+int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2,
+                    const void* residual, int T, int h, int f, int dtype, void* y, void* saved,
+                    void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t moe_ffn_saved_bytes(int T, int f);
+size_t moe_ffn_forward_workspace(int T, int h, int f);
+
+/*
+ * Gradients of moe_ffn_forward from dy and what the forward call saved:
+ *   da = dy W2,  dg = da * u * silu'(g),  du = da * silu(g)
+ *   dx = dg W1 + du W3,  dW1 = dg^T x,  dW3 = du^T x,  dW2 = dy^T a
+ * (the residual's gradient is dy).  dy, dx [T][h], dW1, dW3 [f][h], dW2 [h][f]
+ * device, dtype; a, dg and du are rounded to dtype, each gradient once.  No
+ * gradient may overlap an input or another gradient.  workspace as above, of
+ * moe_ffn_backward_workspace(T, h, f) bytes.  Sums have a fixed order: the same
+ * call gives the same bits.  T = 0 clears the weights' gradients.  Asynchronous.
+ */
+int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* W3, const void* W2,
+                     const void* saved, int T, int h, int f, int dtype, void* dx, void* dW1,
+                     void* dW3, void* dW2, void* workspace, size_t workspace_bytes,
+                     void* cuda_stream);
+size_t moe_ffn_backward_workspace(int T, int h, int f);
+
+/* 0 when no bounded wait inside moe_ffn_forward / moe_ffn_backward has expired on
+ * the current device since the last call of this function, else
+ * MOE_ERR_DEVICE_TIMEOUT (what such a call wrote is not valid).  Synchronises. */
+int moe_operators_status(void);
+
+/*
  * A stack of MoE layers with attention left out:
  *   x_{l+1} = x_l + MoE_l(RMSNorm(x_l)),  l = 0 .. n_layers-1,
  * each layer with its own kept experts and its own betas[l] (host array, NULL

@@ -62,6 +62,15 @@ int moe_test_host_slabs(const moe_layer_t* layer, int T);
  */
 void moe_test_set_free_bytes_limit(long long bytes);
 
+/*
+ * Host side only.  Tile and split that a launch of the feed-forward block takes on a
+ * machine of `pairs` pairs of multiprocessors: launch = 0 gate/up, 1 down,
+ * 2 the activation's gradient, 3 the input's gradient; plan[6] receives rows a CTA
+ * and accumulator, columns of an item, k-splits, row tiles, column tiles, k-blocks
+ * of 64 in the contraction.  Errors: MOE_ERR_INVALID_ARG.
+ */
+int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]);
+
 #ifdef __cplusplus
 }
 #endif

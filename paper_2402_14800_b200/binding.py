@@ -75,6 +75,15 @@ def load_library(path: str | None = None):
     lib.moe_add_rmsnorm_backward_workspace.restype = ctypes.c_size_t
     lib.moe_add_rmsnorm_backward_workspace.argtypes = [ci, ci]
     lib.moe_add_rmsnorm_backward.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, ctypes.c_size_t, vp]
+    cs = ctypes.c_size_t
+    lib.moe_ffn_saved_bytes.restype = cs
+    lib.moe_ffn_saved_bytes.argtypes = [ci, ci]
+    lib.moe_ffn_forward_workspace.restype = cs
+    lib.moe_ffn_forward_workspace.argtypes = [ci, ci, ci]
+    lib.moe_ffn_backward_workspace.restype = cs
+    lib.moe_ffn_backward_workspace.argtypes = [ci, ci, ci]
+    lib.moe_ffn_forward.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, cs, vp]
+    lib.moe_ffn_backward.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, cs, vp]
     lib.moe_stack_forward.argtypes = [ctypes.POINTER(vp), ci, vp, ci, ctypes.POINTER(cf), cf, vp]
     lib.moe_coselection.argtypes = [vp, vp, ci, ctypes.POINTER(ctypes.c_int32)]
     lib.moe_frequency_subset.restype = u32
@@ -89,6 +98,7 @@ def load_library(path: str | None = None):
     lib.moe_test_wait_expiry_pair.argtypes = [vp, ctypes.c_uint, ci]
     lib.moe_test_large_batch.argtypes = [vp, ci, ci]
     lib.moe_test_host_slabs.argtypes = [vp, ci]
+    lib.moe_test_ffn_plan.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(ci)]
     lib.moe_test_set_free_bytes_limit.restype = None
     lib.moe_test_set_free_bytes_limit.argtypes = [ctypes.c_longlong]
     lib.moe_last_error.restype = ctypes.c_char_p
@@ -469,6 +479,73 @@ def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
     _check(lib.moe_add_rmsnorm_backward(dp, ep, sp, tp, gp, T, h, DTYPES[dt], xp,
                                         _operand("dgain", dgain, dt, (h,), index), wp, n, st))
     return dx, dgain
+
+
+def ffn_saved(T: int, f: int, device) -> torch.Tensor:
+    """A buffer for what ``ffn_forward`` saves for ``ffn_backward``: fp32 [T, f, 2]."""
+    return torch.empty((T, f, 2), dtype=torch.float32, device=device)
+
+
+def ffn_forward(x, W1, W3, W2, residual=None, y=None, saved=None, stream=None):
+    """``moe_ffn_forward``: y = (silu(x W1^T) * (x W3^T)) W2^T [+ residual], bf16 or fp16.
+
+    x, residual, y [T, h], W1, W3 [f, h], W2 [h, f].  ``saved``: a buffer of ``ffn_saved`` where
+    ``ffn_backward`` is to follow.  Returns y."""
+    return _on_device_of(x, 2, stream, _ffn_forward, x, W1, W3, W2, residual, y, saved)
+
+
+def _ffn_sizes(x, W1):
+    if not (isinstance(W1, torch.Tensor) and W1.dim() == 2):
+        raise MoeError(-1, "W1 must be a matrix [f, h]")
+    return x.shape[0], x.shape[1], W1.shape[0]
+
+
+def _ffn_forward(index, st, x, W1, W3, W2, residual, y, saved):
+    T, h, f = _ffn_sizes(x, W1)
+    dt, shape = x.dtype, x.shape
+    xp = _operand("x", x, dt, shape, index)
+    w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
+    w2, rp = _operand("W2", W2, dt, (h, f), index), _operand("residual", residual, dt, shape, index)
+    sp = _operand("saved", saved, torch.float32, (T, f, 2), index)
+    if y is None:
+        y = torch.empty_like(x)
+    yp = _operand("y", y, dt, shape, index)
+    lib = load_library()
+    n = lib.moe_ffn_forward_workspace(T, h, f)
+    ws = x.new_empty((n,), dtype=torch.uint8)
+    _check(lib.moe_ffn_forward(xp, w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
+    return y
+
+
+def ffn_backward(d_y, x, W1, W3, W2, saved, dx=None, dW1=None, dW3=None, dW2=None, stream=None):
+    """``moe_ffn_backward``: gradients of ``ffn_forward`` from d_y and its ``saved`` buffer.
+    Returns (dx, dW1, dW3, dW2); the residual's gradient is d_y itself."""
+    return _on_device_of(x, 2, stream, _ffn_backward, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2)
+
+
+def _ffn_backward(index, st, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2):
+    T, h, f = _ffn_sizes(x, W1)
+    dt, shape = x.dtype, x.shape
+    dp, xp = _operand("d_y", d_y, dt, shape, index), _operand("x", x, dt, shape, index)
+    w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
+    w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.float32, (T, f, 2), index)
+    dx = torch.empty_like(x) if dx is None else dx
+    dW1 = torch.empty_like(W1) if dW1 is None else dW1
+    dW3 = torch.empty_like(W3) if dW3 is None else dW3
+    dW2 = torch.empty_like(W2) if dW2 is None else dW2
+    lib = load_library()
+    n = lib.moe_ffn_backward_workspace(T, h, f)
+    ws = x.new_empty((n,), dtype=torch.uint8)
+    _check(lib.moe_ffn_backward(dp, xp, w1, w3, w2, sp, T, h, f, DTYPES[dt], _operand("dx", dx, dt, shape, index),
+                                _operand("dW1", dW1, dt, (f, h), index), _operand("dW3", dW3, dt, (f, h), index),
+                                _operand("dW2", dW2, dt, (h, f), index), ws.data_ptr(), n, st))
+    return dx, dW1, dW3, dW2
+
+
+def operators_status(device=None) -> int:
+    """``moe_operators_status`` of a device (None: the current one)."""
+    with torch.cuda.device(device):
+        return int(load_library().moe_operators_status())
 
 
 def stack_forward(layers, x, betas=None, eps: float = 1e-5, y=None):

@@ -1,0 +1,792 @@
+// Dense gated feed-forward block on the caller's own weights, forward and backward.
+//
+//   forward   g = x W1^T,  u = x W3^T,  a = silu(g) * u            (one launch)
+//             y = a W2^T [+ residual]
+//   backward  da = dy W2,  dg = da * u * silu'(g),  du = da * silu(g)
+//             dx = dg W1 + du W3,   dW1 = dg^T x,  dW3 = du^T x,  dW2 = dy^T a
+//
+// One persistent warp-specialised GEMM does all of it, D[m][n] = sum_k A[m][k] B[n][k], stored as
+// out[n][m]: m is always the contiguous index of the output, so a warp's 32 tensor-memory lanes write
+// neighbouring elements.  What differs between the launches is where A and B come from, how they lie in
+// memory (contiguous in k, or in m / n: the tensor cores take either from a 128-byte swizzled tile), and the
+// epilogue.
+//
+// A pair of CTAs (cluster of two, cta_group::2) computes an item of 4 R x n_tile: two accumulators of M = 256
+// (each CTA holds 128 rows of each, R of them in use) by up to 256 columns, half of them staged by either CTA.
+// In the gate/up launch the accumulators are g and u of the same 2 R features, so a thread holds both and the
+// activation needs no exchange.  The tile follows from the sizes (choose_plan): large problems take 512 x 256
+// per pair, which halves the traffic from L2 that a 256 x 128 tile per CTA would need and that bounds the tensor
+// pipe; a few tokens take as many weight rows a CTA as give every SM the same number of weight bytes, since then
+// HBM is all that counts; and where rows alone do not fill the machine the contraction is split, the partial
+// sums go to fp32 planes and a small kernel adds them in a fixed order.
+//
+// Rounding: sums, g, u and everything in an epilogue are fp32.  a, dg and du are rounded to the tensors' type,
+// because the tensor cores take them as 16-bit operands; g and u are saved for the backward pass in fp32, since
+// rounding them as well would cost the gradients as much again as those operands' roundings do.
+//
+// Waits are bounded and end in the status word of moe_operators_status.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "moe_test_hooks.h"
+#include "operators.h"
+#include "sm100.h"
+
+namespace moe {
+
+namespace {
+
+__device__ int g_status;  // set when a bounded wait of this file's kernels expired
+
+enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kDx, kDw };
+
+constexpr int kEpiWarps = 16;
+constexpr int kGemmThreads = 96 + 32 * kEpiWarps;
+constexpr int kSmemLimit = 230400;      // dynamic shared memory of a CTA, the barrier block lies beside it
+constexpr int kAccRows = 128;           // rows of an accumulator in one CTA
+constexpr int kMaxStages = 8;           // size of the barrier block
+constexpr int kBandTiles = 16;          // n tiles that sweep the m tiles together
+
+// A operand contiguous in m (W2 of da, W1 and W3 of dx, x and a of the weights' gradients); B contiguous in n
+constexpr __host__ __device__ bool a_mn(int kind) { return kind == kDact || kind == kDx || kind == kDw; }
+constexpr __host__ __device__ bool b_mn(int kind) { return kind == kDw; }
+constexpr __host__ __device__ bool gate_up(int kind) { return kind == kGateUp || kind == kGateUpSave; }
+
+struct Problem {
+  int M, N;    // m and n range
+  int mt, nt;  // tiles
+  void* out;   // [N][M]
+};
+
+struct Args {
+  Problem p[3];
+  int np;             // problems of the launch (the three weight gradients), else 1
+  int KB, segKB;      // k-blocks of 64; of one segment (dx: two segments, else segKB = KB)
+  int S, kbs;         // k-splits, k-blocks of each
+  int R, n_tile;      // rows of A a CTA and accumulator loads, columns of an item
+  int stages, slot_a, stage;  // pipeline stages, bytes of an accumulator's A tile, of a stage
+  int fp16;
+  const void* residual;       // kPlain
+  float2* saved;              // [N][M] (g, u): written by kGateUpSave, read by kDact
+  void *dg, *du;              // kDact, beside out = a
+  float* planes;              // S > 1: [S][N][M] partial sums
+};
+
+struct Maps {
+  CUtensorMap a[3], b[3];
+};
+
+__device__ __forceinline__ uint32_t pack16(float a, float b, int fp16) {
+  if (fp16) {
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+  return pack_bf16(a, b);
+}
+__device__ __forceinline__ float2 unpack16(uint32_t v, int fp16) {
+  if (fp16) return __half22float2(*reinterpret_cast<const __half2*>(&v));
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+
+// Descriptor of a tile that is contiguous in m (or n): boxes of 64 elements x 64 k, each 64 rows of 128 bytes;
+// groups of 8 k are 1024 bytes apart (stride offset), boxes 8192 (leading offset).
+__device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
+  d |= (uint64_t)(8192 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+constexpr uint32_t kMnBoxBytes = 64 * 128;
+constexpr uint32_t kStepK = 32 >> 4;            // 16 k further, in descriptor units: 32 bytes along a row
+constexpr uint32_t kStepMn = (16 * 128) >> 4;   // or 16 rows of k
+
+// Both operands of one type, fp16 or bf16 (never mixed), fp32 accumulation; bits 15 and 16: A, B contiguous in m, n.
+__device__ __forceinline__ uint32_t idesc16(int M, int N, int fp16, bool amn, bool bmn) {
+  const uint32_t t = fp16 ? 0u : 1u;
+  return (1u << 4) | (t << 7) | (t << 10) | ((amn ? 1u : 0u) << 15) | ((bmn ? 1u : 0u) << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+struct Item {
+  int prob, m0, n0, ks, kb0, kb1;  // m0: first row of the pair's item
+  int valid;                       // columns that exist
+};
+
+// Items of a problem: k-split -> band of at most kBandTiles n tiles -> m tile -> n tile, so that the items in
+// flight share few tiles of either operand in L2.
+template <int KIND> __device__ __forceinline__ Item decode_item(const Args& a, int item) {
+  Item t;
+  t.prob = 0;
+  if (KIND == kDw) {
+    while (t.prob + 1 < a.np && item >= a.p[t.prob].mt * a.p[t.prob].nt) {
+      item -= a.p[t.prob].mt * a.p[t.prob].nt;
+      ++t.prob;
+    }
+  }
+  const Problem& p = a.p[t.prob];
+  t.ks = KIND == kDw || gate_up(KIND) ? 0 : item / (p.mt * p.nt);
+  item -= t.ks * p.mt * p.nt;
+  const int bands = (p.nt + kBandTiles - 1) / kBandTiles;
+  const int per_band = (p.nt + bands - 1) / bands;
+  const int band = item / (per_band * p.mt);
+  const int rem = item - band * per_band * p.mt;
+  const int band_tiles = min(per_band, p.nt - band * per_band);
+  const int m = rem / band_tiles;
+  t.m0 = m * (gate_up(KIND) ? 2 : 4) * a.R;
+  t.n0 = (band * per_band + rem - m * band_tiles) * a.n_tile;
+  t.valid = min(a.n_tile, p.N - t.n0);
+  t.kb0 = t.ks * a.kbs;
+  t.kb1 = min(a.KB, t.kb0 + a.kbs);
+  return t;
+}
+
+// Stores 16 columns n (col0 .. col0 + 15 of the item) of the warp's 32 neighbouring m, given as 8 packed pairs of
+// columns per lane: even lanes take the even columns of two neighbouring m, odd lanes the odd ones.
+// `out` points at (n of col0, m of lane 0); in_m: this lane's pair of m exists.
+__device__ __forceinline__ void store_cols(const uint32_t* v, uint16_t* out, long long ld, int col0, int valid, bool in_m,
+                                           int lane) {
+  const bool odd = lane & 1;
+  uint16_t* o = out + (lane & 30) + (odd ? ld : 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, v[i], 1);
+    const uint32_t w = odd ? __byte_perm(other, v[i], 0x7632) : __byte_perm(v[i], other, 0x5410);
+    if (in_m && col0 + 2 * i + (lane & 1) < valid) *reinterpret_cast<uint32_t*>(o) = w;
+    o += 2 * ld;
+  }
+}
+
+__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+
+template <int KIND>
+__global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Bars bars;
+  constexpr bool AMN = a_mn(KIND), BMN = b_mn(KIND), GU = gate_up(KIND);
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();  // 0 = leader of the pair
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+
+  setup_barriers<kMaxStages>(bars, 2 * kEpiWarps, 2);
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&bars.tmem_base), 512);
+    tmem_relinquish_pair();
+  }
+  pdl_launch_dependents();
+  pdl_wait();
+  __syncwarp();
+  tc_fence_before();
+  cluster_sync_all();  // both CTAs' barriers exist before anything is signalled across the pair
+  tc_fence_after();
+  const uint32_t tmem_base = *(volatile uint32_t*)&bars.tmem_base;
+  volatile int* abort_flag = &bars.abort_flag;
+
+  const uint32_t ns = (uint32_t)args.stages, stage_bytes = (uint32_t)args.stage, slot_a = (uint32_t)args.slot_a;
+  const int half = args.n_tile >> 1;  // a multiple of 16
+  int n_items = 0;
+  for (int p = 0; p < (KIND == kDw ? args.np : 1); ++p) n_items += args.p[p].mt * args.p[p].nt;
+  if (KIND != kDw && !GU) n_items *= args.S;
+  uint32_t issued = 0;
+
+  if (warp == 0) {
+    // ---- TMA producer of this CTA's rows of A and its half of the columns; the bytes of both CTAs are counted on
+    // the leader's barrier
+    const uint32_t a_bytes = AMN ? (uint32_t)((args.R + 63) >> 6) * kMnBoxBytes : (uint32_t)args.R * 128u;
+    const uint32_t b_bytes = BMN ? (uint32_t)((half + 63) >> 6) * kMnBoxBytes : (uint32_t)half * 128u;
+    const uint32_t bytes = 2u * (2u * a_bytes + b_bytes);
+    uint32_t s = 0, ph = 0;
+    bool ok = true;
+    for (int item = pair; item < n_items && ok; item += n_pairs) {
+      const Item t = decode_item<KIND>(args, item);
+      const int row0 = t.m0 + args.R * (int)rank, col0 = t.n0 + half * (int)rank;
+      for (int kb = t.kb0; kb < t.kb1; ++kb, ++issued) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.empty[s]), ph ^ 1u, abort_flag));
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t full = map_to_cta(smem_u32(&bars.full[s]), 0);
+          const uint32_t sa = smem_base + s * stage_bytes;
+          if (rank == 0) mbar_expect_tx(smem_u32(&bars.full[s]), bytes);
+          const int seg = KIND == kDx && kb >= args.segKB ? 1 : 0;
+          const int k0 = (kb - seg * args.segKB) * BK;
+#pragma unroll
+          for (int acc = 0; acc < 2; ++acc) {
+            const CUtensorMap* map = &maps.a[GU ? acc : KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
+            const int row = GU ? row0 : row0 + 2 * args.R * acc;
+            if (AMN) {
+              for (int j = 0; j < args.R; j += 64) tma_load_2d_pair(sa + acc * slot_a + j * 128, map, row + j, k0, full);
+            } else {
+              tma_load_2d_pair(sa + acc * slot_a, map, k0, row, full);
+            }
+          }
+          const CUtensorMap* map = &maps.b[KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
+          if (BMN) {
+            for (int j = 0; j < half; j += 64) tma_load_2d_pair(sa + 2 * slot_a + j * 128, map, col0 + j, k0, full);
+          } else {
+            tma_load_2d_pair(sa + 2 * slot_a, map, k0, col0, full);
+          }
+        }
+        if (++s == ns) { s = 0; ph ^= 1u; }
+        __syncwarp();
+      }
+    }
+  } else if (warp <= 2) {
+    // ---- MMA issuers of the leader, one warp per accumulator
+    if (rank == 0) {
+      const uint32_t acc = (uint32_t)warp - 1u;
+      const uint32_t d_tmem = tmem_base + 256u * acc;
+      const uint32_t tmem_full = smem_u32(&bars.tmem_full[acc]), tmem_empty = smem_u32(&bars.tmem_empty[acc]);
+      const uint32_t idesc = idesc16(256, args.n_tile, args.fp16, AMN, BMN);
+      constexpr uint32_t sa_k = AMN ? kStepMn : kStepK, sb_k = BMN ? kStepMn : kStepK;
+      uint32_t s = 0, ph = 0, nu = 0;  // nu: items so far
+      bool ok = true;
+      for (int item = pair; item < n_items && ok; item += n_pairs, ++nu) {
+        const Item t = decode_item<KIND>(args, item);
+        for (int kb = t.kb0; kb < t.kb1; ++kb) {
+          bool ready = mbar_wait(smem_u32(&bars.full[s]), ph, abort_flag);
+          if (kb == t.kb0) ready = ready && mbar_wait(tmem_empty, (nu & 1u) ^ 1u, abort_flag);
+          ok = __all_sync(0xffffffffu, ready);
+          if (!ok) break;
+          tc_fence_after();
+          if (lane == 0) {
+            const uint32_t sa = smem_base + s * stage_bytes + acc * slot_a, sb = smem_base + s * stage_bytes + 2 * slot_a;
+            const uint64_t adesc = AMN ? smem_desc_mn128(sa) : smem_desc_k128(sa);
+            const uint64_t bdesc = BMN ? smem_desc_mn128(sb) : smem_desc_k128(sb);
+            umma_bf16_pair(d_tmem, adesc, bdesc, idesc, kb > t.kb0 ? 1u : 0u);
+            umma_bf16_pair(d_tmem, adesc + sa_k, bdesc + sb_k, idesc, 1u);
+            umma_bf16_pair(d_tmem, adesc + 2 * sa_k, bdesc + 2 * sb_k, idesc, 1u);
+            umma_bf16_pair(d_tmem, adesc + 3 * sa_k, bdesc + 3 * sb_k, idesc, 1u);
+            umma_commit_pair(smem_u32(&bars.empty[s]));
+            if (kb == t.kb1 - 1) umma_commit_pair(tmem_full);
+          }
+          if (++s == ns) { s = 0; ph ^= 1u; }
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    // ---- epilogue: warp w reads tensor-memory lanes 32 (w % 4) .. + 31, and of the chunks of 16 columns every fourth
+    const int wq = warp & 3, group = (warp - 3) >> 2;
+    const int row = 32 * wq + lane;  // row of this thread in its CTA's part of an accumulator
+    const uint32_t empty0 = map_to_cta(smem_u32(&bars.tmem_empty[0]), 0);
+    const uint32_t empty1 = map_to_cta(smem_u32(&bars.tmem_empty[1]), 0);
+    const uint32_t taddr0 = tmem_base + ((uint32_t)(32 * wq) << 16);
+    const int fp16 = args.fp16;
+    uint32_t nu = 0;
+    bool ok = true;
+    for (int item = pair; item < n_items && ok; item += n_pairs, ++nu) {
+      const Item t = decode_item<KIND>(args, item);
+      const Problem& p = args.p[t.prob];
+      const long long ld = p.M;
+      if constexpr (GU) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[0]), nu & 1u, abort_flag) &&
+                                         mbar_wait(smem_u32(&bars.tmem_full[1]), nu & 1u, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const int m0 = t.m0 + args.R * (int)rank + 32 * wq;  // of lane 0
+        const bool in_m = row < args.R && m0 + lane < p.M;
+        uint32_t act[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c0 = 16 * (group + 4 * i);
+          if (c0 >= t.valid) continue;
+          uint32_t g[16], u[16];
+          tmem_ld16(taddr0 + c0, g);
+          tmem_ld16(taddr0 + 256 + c0, u);
+          tmem_ld_wait();
+          if constexpr (KIND == kGateUpSave) {
+            float2* o = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              if (in_m && c0 + c < t.valid) *o = make_float2(__uint_as_float(g[c]), __uint_as_float(u[c]));
+              o += ld;
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+            act[i][c] = pack16(silu_mul(__uint_as_float(g[2 * c]), __uint_as_float(u[2 * c])),
+                               silu_mul(__uint_as_float(g[2 * c + 1]), __uint_as_float(u[2 * c + 1])), fp16);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive_cluster(empty0);
+          mbar_arrive_cluster(empty1);
+        }
+        // R and M are even, so both m of a lane's pair exist or neither
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c0 = 16 * (group + 4 * i);
+          if (c0 >= t.valid) continue;
+          store_cols(act[i], reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
+        }
+      } else {
+#pragma unroll 1
+        for (int acc = 0; acc < 2; ++acc) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t taddr = taddr0 + 256 * acc;
+          const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
+          const bool in_m = row < args.R && m0 + lane < p.M;
+          if (KIND != kDact || args.S > 1) {
+            // everything this warp wants of the accumulator goes to registers, and the accumulator back to the
+            // MMAs, before the stores
+            uint32_t v[4][16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tmem_ld16(taddr + 16 * (group + 4 * i), v[i]);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int c0 = 16 * (group + 4 * i);
+              if (c0 >= t.valid) continue;
+              const long long at = (long long)(t.n0 + c0) * ld + m0;
+              if (KIND != kDw && args.S > 1) {
+                float* o = args.planes + (long long)t.ks * p.N * ld + at + lane;
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                  if (in_m && c0 + c < t.valid) *o = __uint_as_float(v[i][c]);
+                  o += ld;
+                }
+              } else {
+                if (KIND == kPlain && args.residual) {  // y itself, maybe: a store carries only what was added before
+                  const uint16_t* r = reinterpret_cast<const uint16_t*>(args.residual) + at + lane;
+#pragma unroll
+                  for (int c = 0; c < 16; ++c) {
+                    if (in_m && c0 + c < t.valid)
+                      v[i][c] = __float_as_uint(__uint_as_float(v[i][c]) + unpack16(__ldcg(r), fp16).x);
+                    r += ld;
+                  }
+                }
+                uint32_t w[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                  w[c] = pack16(__uint_as_float(v[i][2 * c]), __uint_as_float(v[i][2 * c + 1]), fp16);
+                store_cols(w, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+              }
+            }
+          } else {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+              const int c0 = 16 * (group + 4 * i);
+              if (c0 >= t.valid) continue;
+              const long long at = (long long)(t.n0 + c0) * ld + m0;
+              float2 gu[16];
+              const float2* sp = args.saved + at + lane;
+#pragma unroll
+              for (int c = 0; c < 16; ++c) {
+                gu[c] = in_m && c0 + c < t.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
+                sp += ld;
+              }
+              uint32_t v[16], wa[8], wg[8], wu[8];
+              tmem_ld16(taddr + c0, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                float a2[2], g2[2], u2[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                  const float g = gu[2 * c + q].x, u = gu[2 * c + q].y, da = __uint_as_float(v[2 * c + q]);
+                  const float sg = sigmoid(g), sw = g * sg;
+                  a2[q] = silu_mul(g, u);  // the forward pass's bits
+                  g2[q] = da * u * fmaf(sw, 1.0f - sg, sg);
+                  u2[q] = da * sw;
+                }
+                wa[c] = pack16(a2[0], a2[1], fp16);
+                wg[c] = pack16(g2[0], g2[1], fp16);
+                wu[c] = pack16(u2[0], u2[1], fp16);
+              }
+              store_cols(wa, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+              store_cols(wg, reinterpret_cast<uint16_t*>(args.dg) + at, ld, c0, t.valid, in_m, lane);
+              store_cols(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+          }
+        }
+      }
+    }
+  }
+
+  teardown_pair(bars, tmem_base, 512, issued, ns, rank, &g_status);
+}
+
+// Sum of the S planes of a split launch in their order, and what the epilogue would have done with it: four
+// neighbouring m a thread.
+template <bool DACT>
+__global__ void __launch_bounds__(256) ffn_join_kernel(const float* planes, int S, long long n, const void* residual,
+                                                       const float2* saved, void* out, void* dg, void* du, int fp16) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  float4 v = ld_l2(reinterpret_cast<const float4*>(planes + i));
+  for (int s = 1; s < S; ++s) {
+    const float4 w = ld_l2(reinterpret_cast<const float4*>(planes + (long long)s * n + i));
+    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+  }
+  if constexpr (!DACT) {
+    if (residual) {
+      const uint2 r = __ldcg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(residual) + i));
+      const float2 r0 = unpack16(r.x, fp16), r1 = unpack16(r.y, fp16);
+      v.x += r0.x; v.y += r0.y; v.z += r1.x; v.w += r1.y;
+    }
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) =
+        make_uint2(pack16(v.x, v.y, fp16), pack16(v.z, v.w, fp16));
+  } else {
+    const float4 s0 = ld_l2(reinterpret_cast<const float4*>(saved + i)), s1 = ld_l2(reinterpret_cast<const float4*>(saved + i) + 1);
+    const float g[4] = {s0.x, s0.z, s1.x, s1.z}, u[4] = {s0.y, s0.w, s1.y, s1.w}, da[4] = {v.x, v.y, v.z, v.w};
+    float a4[4], g4[4], u4[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float sg = sigmoid(g[q]), sw = g[q] * sg;
+      a4[q] = silu_mul(g[q], u[q]);
+      g4[q] = da[q] * u[q] * fmaf(sw, 1.0f - sg, sg);
+      u4[q] = da[q] * sw;
+    }
+    auto put = [&](void* o, const float* f) {
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(o) + i) =
+          make_uint2(pack16(f[0], f[1], fp16), pack16(f[2], f[3], fp16));
+    };
+    put(out, a4);
+    put(dg, g4);
+    put(du, u4);
+  }
+}
+
+// ------------------------------------------------------------------------------ host
+
+struct Plan {
+  int R, n_tile, S, mt, nt;
+};
+
+// Tile and split of a launch of M x N outputs and KB k-blocks, by a model in SM cycles: an item's k-block takes what
+// bounds it, the tensor pipe (N / 2 cycles for each of 8 MMAs) or the bytes that a CTA draws from L2 (about 36 a
+// cycle with every SM drawing); an item has a fixed part and an epilogue; items are dealt to the pairs in rounds; a
+// split launch writes and reads planes.  Among equals the earlier, larger tile.
+Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
+  const int unit = gate_up(kind) ? 2 : 4;
+  Plan best = {};
+  double best_cost = 1e300;
+  for (int cols = 256; cols >= 32; cols -= 32) {
+    const int nt = (N + cols - 1) / cols;
+    const int n_tile = ((N + nt - 1) / nt + 31) / 32 * 32;
+    if (n_tile != cols) continue;  // the same tiles with fewer columns come later
+    for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4)); ++S) {
+      const int kbs = (KB + S - 1) / S;
+      if ((KB + kbs - 1) / kbs != S) continue;
+      const int mt_min = (M + unit * kAccRows - 1) / (unit * kAccRows);
+      const int least = (mt_min * nt * S + pairs - 1) / pairs;
+      for (int rounds = least; rounds <= least + 1; ++rounds) {
+        int R, mt;
+        if (a_mn(kind)) {
+          R = rounds == least ? 128 : 64;
+        } else {
+          const int most = rounds * pairs / (nt * S);
+          if (most < 1) continue;
+          R = ((M + unit * most - 1) / (unit * most) + 1) / 2 * 2;
+          if (R < 8) R = 8;
+          if (R > kAccRows) R = kAccRows;
+        }
+        mt = (M + unit * R - 1) / (unit * R);
+        const int r = (mt * nt * S + pairs - 1) / pairs;
+        const double bytes = 2.0 * ((R + 7) / 8 * 8) * 128 + n_tile / 2 * 128.0;
+        const double kb = std::max(4.0 * n_tile, bytes / 36.0);
+        double cost = r * (kbs * kb + 2000.0 + 10.0 * n_tile);
+        if (S > 1) cost += 3000.0 + (double)S * N * M * 8 / (148 * 20.0);
+        if (cost < best_cost) {
+          best_cost = cost;
+          best = {R, n_tile, S, mt, nt};
+        }
+      }
+    }
+  }
+  return best;
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
+  a.slot_a = a_mn(KIND) ? (a.R + 63) / 64 * (int)kMnBoxBytes : (a.R + 7) / 8 * 1024;
+  const int half = a.n_tile / 2;
+  const int slot_b = b_mn(KIND) ? (half + 63) / 64 * (int)kMnBoxBytes : half * 128;
+  a.stage = 2 * a.slot_a + slot_b;
+  // an MMA reads 128 rows of A (and whole boxes of columns) whatever was loaded: up to 32 KB behind the last slot
+  const int tail = std::max(0, kAccRows * 128 - a.slot_a);
+  a.stages = std::min(kMaxStages, (kSmemLimit - 1024 - tail) / a.stage);
+  a.kbs = (a.KB + a.S - 1) / a.S;
+  int items = 0;
+  for (int p = 0; p < a.np; ++p) items += a.p[p].mt * a.p[p].nt;
+  items *= a.S;
+  static std::atomic<unsigned long long> set{0};  // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !(set.load() >> dev & 1)) {
+    e = cudaFuncSetAttribute(ffn_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) set.fetch_or(1ull << dev);
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * std::min(items, pairs));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = 1024 + (size_t)a.stages * a.stage + tail;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<KIND>, maps, a);
+}
+
+cudaError_t launch_join(bool dact, const Args& a, cudaStream_t st) {
+  const long long n = (long long)a.p[0].M * a.p[0].N;
+  const dim3 grid((unsigned)((n / 4 + 255) / 256));
+  if (dact)
+    return launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, (const void*)nullptr,
+                      (const float2*)a.saved, a.p[0].out, a.dg, a.du, a.fp16);
+  return launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, a.residual,
+                    (const float2*)nullptr, a.p[0].out, (void*)nullptr, (void*)nullptr, a.fp16);
+}
+
+Args args_of(const Plan& p, int M, int N, int KB, void* out, int dtype) {
+  Args a = {};
+  a.p[0] = {M, N, p.mt, p.nt, out};
+  a.np = 1;
+  a.KB = a.segKB = KB;
+  a.S = p.S;
+  a.R = p.R;
+  a.n_tile = p.n_tile;
+  a.fp16 = dtype == MOE_FP16;
+  return a;
+}
+
+// Tensor map of one operand: contiguous in k ([rows][K]), boxes of 64 k x box rows, or in m / n ([K][rows]), boxes of
+// 64 rows x 64 k.
+int map_k(CUtensorMap* m, const void* base, int K, int rows, int box) { return make_map_2d(m, base, K, rows, box); }
+int map_mn(CUtensorMap* m, const void* base, int rows, int K) { return make_map_2d(m, base, rows, K, BK); }
+
+int kblocks(int K) { return (K + BK - 1) / BK; }
+
+Plan gu_plan(int T, int h, int f, int pairs) { return choose_plan(kGateUp, f, T, kblocks(h), false, pairs); }
+Plan down_plan(int T, int h, int f, int pairs) { return choose_plan(kPlain, h, T, kblocks(f), true, pairs); }
+Plan dact_plan(int T, int h, int f, int pairs) { return choose_plan(kDact, f, T, kblocks(h), true, pairs); }
+Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kDx, h, T, 2 * kblocks(f), true, pairs); }
+
+size_t plane_bytes(const Plan& p, int T, int M) { return p.S > 1 ? round256((size_t)p.S * T * M * sizeof(float)) : 0; }
+
+int check_block(int T, int h, int f, int dtype) {
+  if (dtype != MOE_BF16 && dtype != MOE_FP16)
+    return set_error(MOE_ERR_INVALID_ARG, "dtype = %d is neither MOE_BF16 nor MOE_FP16", dtype);
+  if (T < 0 || T > kMaxOperatorTokens) return set_error(MOE_ERR_INVALID_ARG, "T = %d outside 0..%d", T, kMaxOperatorTokens);
+  if (h < 8 || f < 8 || h % 8 || f % 8 || h > (1 << 20) || f > (1 << 20))
+    return set_error(MOE_ERR_UNSUPPORTED_SHAPE, "h = %d and f = %d must be multiples of 8 in 8..%d", h, f, 1 << 20);
+  return MOE_OK;
+}
+
+// once per device: the current device can run the kernels, the driver's encoder is there
+int check_device() {
+  static std::atomic<unsigned long long> good{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return set_error(MOE_ERR_CUDA, "cudaGetDevice: %s", cudaGetErrorString(e));
+  if (dev < 64 && (good.load() >> dev & 1)) return MOE_OK;
+  int major = 0;
+  e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+  if (e != cudaSuccess) return set_error(MOE_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
+  if (major != 10) return set_error(MOE_ERR_ARCH, "device has compute capability %d.x, sm_100 is required", major);
+  if (gemm_init_driver_api()) return set_error(MOE_ERR_CUDA, "cuTensorMapEncodeTiled not available");
+  if (dev < 64) good.fetch_or(1ull << dev);
+  return MOE_OK;
+}
+
+#define FFN_TRY(what, expr)                                                                             \
+  do {                                                                                                  \
+    const cudaError_t e_ = (expr);                                                                      \
+    if (e_ != cudaSuccess) return set_error(MOE_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e_));      \
+  } while (0)
+#define FFN_MAP(expr)                                                                    \
+  do {                                                                                   \
+    if (expr) return set_error(MOE_ERR_CUDA, "building a tensor map failed: " #expr);    \
+  } while (0)
+
+}  // namespace
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" {
+
+size_t moe_ffn_saved_bytes(int T, int f) {
+  if (T < 1 || T > kMaxOperatorTokens || f < 8 || f % 8 || f > (1 << 20)) return 0;
+  return (size_t)T * f * sizeof(float2);
+}
+
+size_t moe_ffn_forward_workspace(int T, int h, int f) {
+  if (T < 1 || check_block(T, h, f, MOE_BF16)) return 0;
+  return round256((size_t)T * f * 2) + plane_bytes(down_plan(T, h, f, sm_count() / 2), T, h);
+}
+
+size_t moe_ffn_backward_workspace(int T, int h, int f) {
+  if (T < 1 || check_block(T, h, f, MOE_BF16)) return 0;
+  const int pairs = sm_count() / 2;
+  return 3 * round256((size_t)T * f * 2) +
+         std::max(plane_bytes(dact_plan(T, h, f, pairs), T, f), plane_bytes(dx_plan(T, h, f, pairs), T, h));
+}
+
+int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2, const void* residual, int T, int h, int f,
+                    int dtype, void* y, void* saved, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_block(T, h, f, dtype);
+  if (rc) return rc;
+  if (T == 0) return MOE_OK;
+  if (!x || !W1 || !W3 || !W2 || !y) return set_error(MOE_ERR_INVALID_ARG, "x, W1, W3, W2 or y is NULL");
+  if (!aligned16(x) || !aligned16(W1) || !aligned16(W3) || !aligned16(W2) || !aligned16(residual) || !aligned16(y) ||
+      !aligned16(saved) || !aligned16(workspace))
+    return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  const size_t n = (size_t)T * h * 2, w = (size_t)h * f * 2, n_saved = (size_t)T * f * sizeof(float2);
+  if (overlap(y, n, x, n) || overlap(y, n, W1, w) || overlap(y, n, W3, w) || overlap(y, n, W2, w) ||
+      overlap(y, n, saved, n_saved) || (residual != y && overlap(y, n, residual, n)))
+    return set_error(MOE_ERR_INVALID_ARG, "y overlaps another tensor (only the residual itself is allowed)");
+  const size_t need = moe_ffn_forward_workspace(T, h, f);
+  if (!workspace || workspace_bytes < need)
+    return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need);
+  if ((rc = check_device())) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int pairs = sm_count() / 2;
+  char* ws = static_cast<char*>(workspace);
+  void* act = ws;
+  Plan p = gu_plan(T, h, f, pairs);
+  Args a = args_of(p, f, T, kblocks(h), act, dtype);
+  a.saved = static_cast<float2*>(saved);
+  Maps maps = {};
+  FFN_MAP(map_k(&maps.a[0], W1, h, f, p.R));
+  FFN_MAP(map_k(&maps.a[1], W3, h, f, p.R));
+  FFN_MAP(map_k(&maps.b[0], x, h, T, p.n_tile / 2));
+  FFN_TRY("gate/up launch", saved ? launch_gemm<kGateUpSave>(maps, a, pairs, st) : launch_gemm<kGateUp>(maps, a, pairs, st));
+  p = down_plan(T, h, f, pairs);
+  a = args_of(p, h, T, kblocks(f), y, dtype);
+  a.residual = residual;
+  a.planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
+  FFN_MAP(map_k(&maps.a[0], W2, f, h, p.R));
+  FFN_MAP(map_k(&maps.b[0], act, f, T, p.n_tile / 2));
+  FFN_TRY("down launch", launch_gemm<kPlain>(maps, a, pairs, st));
+  if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
+  return MOE_OK;
+}
+
+int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* W3, const void* W2, const void* saved, int T,
+                     int h, int f, int dtype, void* dx, void* dW1, void* dW3, void* dW2, void* workspace,
+                     size_t workspace_bytes, void* cuda_stream) {
+  int rc = check_block(T, h, f, dtype);
+  if (rc) return rc;
+  const size_t n = (size_t)T * h * 2, w = (size_t)h * f * 2;
+  if (!dW1 || !dW3 || !dW2) return set_error(MOE_ERR_INVALID_ARG, "dW1, dW3 or dW2 is NULL");
+  if (!aligned16(dW1) || !aligned16(dW3) || !aligned16(dW2))
+    return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  void* outs[4] = {dW1, dW3, dW2, dx};
+  const size_t out_bytes[4] = {w, w, w, n};
+  const void* ins[6] = {dy, x, W1, W3, W2, saved};
+  const size_t in_bytes[6] = {n, n, w, w, w, (size_t)T * f * sizeof(float2)};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 6; ++j)
+      if (overlap(outs[i], out_bytes[i], ins[j], in_bytes[j]))
+        return set_error(MOE_ERR_INVALID_ARG, "a gradient overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(outs[i], out_bytes[i], outs[j], out_bytes[j]))
+        return set_error(MOE_ERR_INVALID_ARG, "two gradients overlap");
+  }
+  if (T == 0) {  // sums of nothing
+    for (int i = 0; i < 3; ++i) FFN_TRY("clearing a gradient", cudaMemsetAsync(outs[i], 0, w, st));
+    return MOE_OK;
+  }
+  if (!dy || !x || !W1 || !W3 || !W2 || !saved || !dx)
+    return set_error(MOE_ERR_INVALID_ARG, "dy, x, W1, W3, W2, saved or dx is NULL");
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(W1) || !aligned16(W3) || !aligned16(W2) || !aligned16(saved) ||
+      !aligned16(dx) || !aligned16(workspace))
+    return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  const size_t need = moe_ffn_backward_workspace(T, h, f);
+  if (!workspace || workspace_bytes < need)
+    return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need);
+  if ((rc = check_device())) return rc;
+  const int pairs = sm_count() / 2;
+  char* ws = static_cast<char*>(workspace);
+  const size_t part = round256((size_t)T * f * 2);
+  void *act = ws, *dg = ws + part, *du = ws + 2 * part;
+  float* planes = reinterpret_cast<float*>(ws + 3 * part);
+  Maps maps = {};
+  // da = dy W2, and a, dg, du
+  Plan p = dact_plan(T, h, f, pairs);
+  Args a = args_of(p, f, T, kblocks(h), act, dtype);
+  a.saved = static_cast<float2*>(const_cast<void*>(saved));
+  a.dg = dg;
+  a.du = du;
+  a.planes = planes;
+  FFN_MAP(map_mn(&maps.a[0], W2, f, h));
+  FFN_MAP(map_k(&maps.b[0], dy, h, T, p.n_tile / 2));
+  FFN_TRY("da launch", launch_gemm<kDact>(maps, a, pairs, st));
+  if (p.S > 1) FFN_TRY("join launch", launch_join(true, a, st));
+  // dx = dg W1 + du W3
+  p = dx_plan(T, h, f, pairs);
+  a = args_of(p, h, T, 2 * kblocks(f), dx, dtype);
+  a.segKB = kblocks(f);
+  a.planes = planes;
+  FFN_MAP(map_mn(&maps.a[0], W1, h, f));
+  FFN_MAP(map_mn(&maps.a[1], W3, h, f));
+  FFN_MAP(map_k(&maps.b[0], dg, f, T, p.n_tile / 2));
+  FFN_MAP(map_k(&maps.b[1], du, f, T, p.n_tile / 2));
+  FFN_TRY("dx launch", launch_gemm<kDx>(maps, a, pairs, st));
+  if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
+  // dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
+  a = args_of({kAccRows, 256, 1, 0, 0}, 0, 0, kblocks(T), nullptr, dtype);
+  a.np = 3;
+  const int rows = 4 * a.R;
+  a.p[0] = {h, f, (h + rows - 1) / rows, (f + a.n_tile - 1) / a.n_tile, dW1};
+  a.p[1] = {h, f, a.p[0].mt, a.p[0].nt, dW3};
+  a.p[2] = {f, h, (f + rows - 1) / rows, (h + a.n_tile - 1) / a.n_tile, dW2};
+  FFN_MAP(map_mn(&maps.a[0], x, h, T));
+  FFN_MAP(map_mn(&maps.a[2], act, f, T));
+  FFN_MAP(map_mn(&maps.b[0], dg, f, T));
+  FFN_MAP(map_mn(&maps.b[1], du, f, T));
+  FFN_MAP(map_mn(&maps.b[2], dy, h, T));
+  maps.a[1] = maps.a[0];
+  FFN_TRY("weight gradients launch", launch_gemm<kDw>(maps, a, pairs, st));
+  return MOE_OK;
+}
+
+int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]) {
+  if (T < 1 || pairs < 1 || !plan || launch < 0 || launch > 3 || check_block(T, h, f, MOE_BF16))
+    return set_error(MOE_ERR_INVALID_ARG, "bad launch, sizes or pairs");
+  const Plan p = launch == 0   ? gu_plan(T, h, f, pairs)
+                 : launch == 1 ? down_plan(T, h, f, pairs)
+                 : launch == 2 ? dact_plan(T, h, f, pairs)
+                               : dx_plan(T, h, f, pairs);
+  const int kb = launch == 0 || launch == 2 ? kblocks(h) : kblocks(f) * (launch == 3 ? 2 : 1);
+  const int v[6] = {p.R, p.n_tile, p.S, p.mt, p.nt, kb};
+  for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  return MOE_OK;
+}
+
+int moe_operators_status(void) {
+  int v = 0, zero = 0;
+  FFN_TRY("reading the status", cudaMemcpyFromSymbol(&v, g_status, sizeof(v)));
+  if (!v) return MOE_OK;
+  FFN_TRY("clearing the status", cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)));
+  return set_error(MOE_ERR_DEVICE_TIMEOUT, "a bounded wait inside a kernel expired");
+}
+
+}  // extern "C"

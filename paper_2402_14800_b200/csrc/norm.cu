@@ -19,7 +19,7 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
-#include "common.h"
+#include "operators.h"
 
 namespace moe {
 
@@ -491,17 +491,6 @@ __global__ void __launch_bounds__(1024) dgain_reduce_kernel(const float* partial
   if (tx == 0 && blockIdx.x * 32 + ty < h) dgain[blockIdx.x * 32 + ty] = from_f<T>(acc);
 }
 
-int sm_count() {
-  static int n[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (!n[dev]) {
-    int v = 0;
-    n[dev] = cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && v > 0 ? v : 148;
-  }
-  return n[dev];
-}
-
 // How a row is cut: threads a row and vectors a thread.
 struct Cut { int tpr, nv; };
 Cut cut_of(int h, int E) {
@@ -588,23 +577,13 @@ template <typename T> cudaError_t launch_bwd_type(NormBwdArgs a, void* dgain, fl
   return launch_pdl(dgain_reduce_kernel<T>, dim3((a.h + 31) / 32), dim3(1024), 0, st, (const float*)partial, n, a.h, (T*)dgain);
 }
 
-bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-constexpr int kMaxTokens = 1 << 24;
 constexpr int kMaxH = 1 << 20;
-
-int element_size(int dtype) { return dtype == MOE_FP32 ? 4 : dtype == MOE_BF16 || dtype == MOE_FP16 ? 2 : 0; }
 
 int check_sizes(int T, int h, int dtype) {
   if (!element_size(dtype)) return set_error(MOE_ERR_INVALID_ARG, "dtype = %d is none of MOE_BF16, MOE_FP16, MOE_FP32", dtype);
-  if (T < 0 || T > kMaxTokens) return set_error(MOE_ERR_INVALID_ARG, "T = %d outside 0..%d", T, kMaxTokens);
+  if (T < 0 || T > kMaxOperatorTokens) return set_error(MOE_ERR_INVALID_ARG, "T = %d outside 0..%d", T, kMaxOperatorTokens);
   if (h < 1 || h > kMaxH) return set_error(MOE_ERR_UNSUPPORTED_SHAPE, "h = %d outside 1..%d", h, kMaxH);
   return MOE_OK;
-}
-
-// [p, p + n) against [q, q + m)
-bool overlap(const void* p, size_t n, const void* q, size_t m) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return p && q && a < b + m && b < a + n;
 }
 
 int forward(const void* x, const void* residual, const void* gain, int T, int h, float eps, int dtype, int group, void* out,
@@ -619,7 +598,7 @@ int forward(const void* x, const void* residual, const void* gain, int T, int h,
   if (q && !scales) return set_error(MOE_ERR_INVALID_ARG, "scales is NULL");
   if ((residual == nullptr) != (s == nullptr))
     return set_error(MOE_ERR_INVALID_ARG, "residual and s go together: both or neither");
-  if (!aligned(x) || !aligned(residual) || !aligned(gain) || !aligned(out) || !aligned(s))
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(out) || !aligned16(s))
     return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
   const size_t e = (size_t)element_size(dtype), n = (size_t)T * h * e;
   const size_t n_out = q ? (size_t)T * h : n;
@@ -659,7 +638,7 @@ int moe_add_rmsnorm_e4m3(const void* x, const void* residual, const void* gain, 
 }
 
 size_t moe_add_rmsnorm_backward_workspace(int T, int h) {
-  if (T < 1 || T > kMaxTokens || h < 1 || h > kMaxH) return 0;
+  if (T < 1 || T > kMaxOperatorTokens || h < 1 || h > kMaxH) return 0;
   const int blocks = sm_count() * kBlocksPerSm;
   const int n = T < blocks ? T : blocks;
   return (size_t)(n > dgain_rows(T) ? n : dgain_rows(T)) * h * sizeof(float);
@@ -672,7 +651,7 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
   if (rc) return rc;
   const size_t e = (size_t)element_size(dtype), n = (size_t)T * h * e;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (!aligned(dgain) || !aligned(workspace)) return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  if (!aligned16(dgain) || !aligned16(workspace)) return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
   if (T == 0) {  // no rows: the gradient of the gain is a sum of nothing
     if (dgain) {
       const cudaError_t err = cudaMemsetAsync(dgain, 0, h * e, st);
@@ -681,7 +660,7 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
     return MOE_OK;
   }
   if (!d_out || !s || !rstd || !dx) return set_error(MOE_ERR_INVALID_ARG, "d_out, s, rstd or dx is NULL");
-  if (!aligned(d_out) || !aligned(d_s) || !aligned(s) || !aligned(gain) || !aligned(dx))
+  if (!aligned16(d_out) || !aligned16(d_s) || !aligned16(s) || !aligned16(gain) || !aligned16(dx))
     return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
   if (dgain && (!workspace || workspace_bytes < moe_add_rmsnorm_backward_workspace(T, h)))
     return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0,
