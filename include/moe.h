@@ -327,7 +327,8 @@ size_t moe_add_rmsnorm_backward_workspace(int T, int h);
  *   MOE_FP16; h and f multiples of 8 in 8 .. 2^20.  residual NULL: 0; y may be the
  *   residual itself, no other overlap is allowed.
  *   saved: NULL, or device memory of moe_ffn_saved_bytes(T, f) bytes that receives
- *   g and u in fp32 ([T][f][2]) for moe_ffn_backward.
+ *   what moe_ffn_backward needs: (u * silu'(g), silu(g)) in fp32 ([T][f][2]), and,
+ *   from the next multiple of 256 bytes on, a in dtype ([T][f]).
  *   workspace: device memory of moe_ffn_forward_workspace(T, h, f) bytes for the
  *   current device, free again when the call's kernels are done; calls that may
  *   run at the same time need one each.

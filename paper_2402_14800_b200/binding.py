@@ -482,8 +482,8 @@ def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
 
 
 def ffn_saved(T: int, f: int, device) -> torch.Tensor:
-    """A buffer for what ``ffn_forward`` saves for ``ffn_backward``: fp32 [T, f, 2]."""
-    return torch.empty((T, f, 2), dtype=torch.float32, device=device)
+    """A buffer for what ``ffn_forward`` saves for ``ffn_backward`` (``moe_ffn_saved_bytes``)."""
+    return torch.empty((int(load_library().moe_ffn_saved_bytes(T, f)),), dtype=torch.uint8, device=device)
 
 
 def ffn_forward(x, W1, W3, W2, residual=None, y=None, saved=None, stream=None):
@@ -506,11 +506,11 @@ def _ffn_forward(index, st, x, W1, W3, W2, residual, y, saved):
     xp = _operand("x", x, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
     w2, rp = _operand("W2", W2, dt, (h, f), index), _operand("residual", residual, dt, shape, index)
-    sp = _operand("saved", saved, torch.float32, (T, f, 2), index)
+    lib = load_library()
+    sp = _operand("saved", saved, torch.uint8, (lib.moe_ffn_saved_bytes(T, f),), index)
     if y is None:
         y = torch.empty_like(x)
     yp = _operand("y", y, dt, shape, index)
-    lib = load_library()
     n = lib.moe_ffn_forward_workspace(T, h, f)
     ws = x.new_empty((n,), dtype=torch.uint8)
     _check(lib.moe_ffn_forward(xp, w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
@@ -528,12 +528,12 @@ def _ffn_backward(index, st, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2):
     dt, shape = x.dtype, x.shape
     dp, xp = _operand("d_y", d_y, dt, shape, index), _operand("x", x, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
-    w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.float32, (T, f, 2), index)
+    lib = load_library()
+    w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.uint8, (lib.moe_ffn_saved_bytes(T, f),), index)
     dx = torch.empty_like(x) if dx is None else dx
     dW1 = torch.empty_like(W1) if dW1 is None else dW1
     dW3 = torch.empty_like(W3) if dW3 is None else dW3
     dW2 = torch.empty_like(W2) if dW2 is None else dW2
-    lib = load_library()
     n = lib.moe_ffn_backward_workspace(T, h, f)
     ws = x.new_empty((n,), dtype=torch.uint8)
     _check(lib.moe_ffn_backward(dp, xp, w1, w3, w2, sp, T, h, f, DTYPES[dt], _operand("dx", dx, dt, shape, index),

@@ -20,9 +20,13 @@
 // HBM is all that counts; and where rows alone do not fill the machine the contraction is split, the partial
 // sums go to fp32 planes and a small kernel adds them in a fixed order.
 //
-// Rounding: sums, g, u and everything in an epilogue are fp32.  a, dg and du are rounded to the tensors' type,
-// because the tensor cores take them as 16-bit operands; g and u are saved for the backward pass in fp32, since
-// rounding them as well would cost the gradients as much again as those operands' roundings do.
+// The forward pass saves what the backward pass makes of g and u: p = u * silu'(g) and q = silu(g), so that
+// dg = da * p and du = da * q, and a itself for dW2.  It has the sigmoid at hand; a second evaluation behind the da
+// products would keep the accumulators from the tensor cores for a quarter of their time.
+//
+// Rounding: sums and everything in an epilogue are fp32.  a, dg and du are rounded to the tensors' type, because the
+// tensor cores take them as 16-bit operands; p and q are saved in fp32, since rounding them as well would cost the
+// gradients as much again as those operands' roundings do.
 //
 // Waits are bounded and end in the status word of moe_operators_status.
 #include <cuda_fp16.h>
@@ -69,9 +73,10 @@ struct Args {
   int stages, slot_a, stage;  // pipeline stages, bytes of an accumulator's A tile, of a stage
   int fp16;
   const void* residual;       // kPlain
-  float2* saved;              // [N][M] (g, u): written by kGateUpSave, read by kDact
-  void *dg, *du;              // kDact, beside out = a
+  float2* saved;              // [N][M] (p, q): written by kGateUpSave, read by kDact
+  void* du;                   // kDact, beside out = dg
   float* planes;              // S > 1: [S][N][M] partial sums
+  int early;                  // A is no earlier launch of this call's output: its first stages may be read ahead
 };
 
 struct Maps {
@@ -100,6 +105,15 @@ __device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr) {
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
   return d;
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 constexpr uint32_t kMnBoxBytes = 64 * 128;
 constexpr uint32_t kStepK = 32 >> 4;            // 16 k further, in descriptor units: 32 bytes along a row
@@ -145,15 +159,16 @@ template <int KIND> __device__ __forceinline__ Item decode_item(const Args& a, i
   return t;
 }
 
-// Stores 16 columns n (col0 .. col0 + 15 of the item) of the warp's 32 neighbouring m, given as 8 packed pairs of
+// Stores 2 PAIRS columns n (from col0 of the item on) of the warp's 32 neighbouring m, given as packed pairs of
 // columns per lane: even lanes take the even columns of two neighbouring m, odd lanes the odd ones.
 // `out` points at (n of col0, m of lane 0); in_m: this lane's pair of m exists.
+template <int PAIRS>
 __device__ __forceinline__ void store_cols(const uint32_t* v, uint16_t* out, long long ld, int col0, int valid, bool in_m,
                                            int lane) {
   const bool odd = lane & 1;
   uint16_t* o = out + (lane & 30) + (odd ? ld : 0);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < PAIRS; ++i) {
     const uint32_t other = __shfl_xor_sync(0xffffffffu, v[i], 1);
     const uint32_t w = odd ? __byte_perm(other, v[i], 0x7632) : __byte_perm(v[i], other, 0x5410);
     if (in_m && col0 + 2 * i + (lane & 1) < valid) *reinterpret_cast<uint32_t*>(o) = w;
@@ -161,7 +176,8 @@ __device__ __forceinline__ void store_cols(const uint32_t* v, uint16_t* out, lon
   }
 }
 
-__device__ __forceinline__ float sigmoid(float g) { return 1.0f / (1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)) by the fast exponential and reciprocal: a few units of the last place, 0 for g below -87
+__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
 template <int KIND>
 __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
@@ -178,8 +194,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
     tmem_alloc_pair(smem_u32(&bars.tmem_base), 512);
     tmem_relinquish_pair();
   }
-  pdl_launch_dependents();
-  pdl_wait();
+  constexpr int kMapsA = KIND == kDw ? 3 : GU || KIND == kDx ? 2 : 1, kMapsB = KIND == kDw ? 3 : KIND == kDx ? 2 : 1;
+  if (warp == 0 && lane < kMapsA) prefetch_tensor_map(&maps.a[lane]);
+  if (warp == 0 && lane >= 8 && lane < 8 + kMapsB) prefetch_tensor_map(&maps.b[lane - 8]);
   __syncwarp();
   tc_fence_before();
   cluster_sync_all();  // both CTAs' barriers exist before anything is signalled across the pair
@@ -188,7 +205,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
   volatile int* abort_flag = &bars.abort_flag;
 
   const uint32_t ns = (uint32_t)args.stages, stage_bytes = (uint32_t)args.stage, slot_a = (uint32_t)args.slot_a;
-  const int half = args.n_tile >> 1;  // a multiple of 16
+  const int half = args.n_tile >> 1;  // a multiple of 8
   int n_items = 0;
   for (int p = 0; p < (KIND == kDw ? args.np : 1); ++p) n_items += args.p[p].mt * args.p[p].nt;
   if (KIND != kDw && !GU) n_items *= args.S;
@@ -202,28 +219,46 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
     const uint32_t bytes = 2u * (2u * a_bytes + b_bytes);
     uint32_t s = 0, ph = 0;
     bool ok = true;
+    auto load_a = [&](const Item& t, int kb, uint32_t stage) {  // and what the stage's barrier expects
+      const uint32_t full = map_to_cta(smem_u32(&bars.full[stage]), 0), sa = smem_base + stage * stage_bytes;
+      if (rank == 0) mbar_expect_tx(smem_u32(&bars.full[stage]), bytes);
+      const int seg = KIND == kDx && kb >= args.segKB ? 1 : 0;
+      const int k0 = (kb - seg * args.segKB) * BK, row0 = t.m0 + args.R * (int)rank;
+#pragma unroll
+      for (int acc = 0; acc < 2; ++acc) {
+        const CUtensorMap* map = &maps.a[GU ? acc : KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
+        const int row = GU ? row0 : row0 + 2 * args.R * acc;
+        if (AMN) {
+          for (int j = 0; j < args.R; j += 64) tma_load_2d_pair(sa + acc * slot_a + j * 128, map, row + j, k0, full);
+        } else {
+          tma_load_2d_pair(sa + acc * slot_a, map, k0, row, full);
+        }
+      }
+    };
+    // The launch before this one let it start after its own wait (below), so everything older than that launch is
+    // complete, the weights among it: the first ring of stages of A may come before the wait.
+    uint32_t ahead = 0;
+    if (args.early && pair < n_items) {
+      const Item t = decode_item<KIND>(args, pair);
+      ahead = min(ns, (uint32_t)(t.kb1 - t.kb0));
+      if (lane == 0)
+        for (uint32_t i = 0; i < ahead; ++i) load_a(t, t.kb0 + (int)i, i);
+      __syncwarp();
+    }
+    pdl_wait();
+    pdl_launch_dependents();
     for (int item = pair; item < n_items && ok; item += n_pairs) {
       const Item t = decode_item<KIND>(args, item);
-      const int row0 = t.m0 + args.R * (int)rank, col0 = t.n0 + half * (int)rank;
+      const int col0 = t.n0 + half * (int)rank;
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++issued) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.empty[s]), ph ^ 1u, abort_flag));
         if (!ok) break;
         if (lane == 0) {
           const uint32_t full = map_to_cta(smem_u32(&bars.full[s]), 0);
           const uint32_t sa = smem_base + s * stage_bytes;
-          if (rank == 0) mbar_expect_tx(smem_u32(&bars.full[s]), bytes);
           const int seg = KIND == kDx && kb >= args.segKB ? 1 : 0;
           const int k0 = (kb - seg * args.segKB) * BK;
-#pragma unroll
-          for (int acc = 0; acc < 2; ++acc) {
-            const CUtensorMap* map = &maps.a[GU ? acc : KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
-            const int row = GU ? row0 : row0 + 2 * args.R * acc;
-            if (AMN) {
-              for (int j = 0; j < args.R; j += 64) tma_load_2d_pair(sa + acc * slot_a + j * 128, map, row + j, k0, full);
-            } else {
-              tma_load_2d_pair(sa + acc * slot_a, map, k0, row, full);
-            }
-          }
+          if (issued >= ahead) load_a(t, kb, s);
           const CUtensorMap* map = &maps.b[KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
           if (BMN) {
             for (int j = 0; j < half; j += 64) tma_load_2d_pair(sa + 2 * slot_a + j * 128, map, col0 + j, k0, full);
@@ -235,6 +270,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
         __syncwarp();
       }
     }
+    issued = max(issued, ahead);
   } else if (warp <= 2) {
     // ---- MMA issuers of the leader, one warp per accumulator
     if (rank == 0) {
@@ -270,6 +306,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
       }
     }
   } else {
+    pdl_wait();
     // ---- epilogue: warp w reads tensor-memory lanes 32 (w % 4) .. + 31, and of the chunks of 16 columns every fourth
     const int wq = warp & 3, group = (warp - 3) >> 2;
     const int row = 32 * wq + lane;  // row of this thread in its CTA's part of an accumulator
@@ -299,18 +336,20 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
           tmem_ld16(taddr0 + c0, g);
           tmem_ld16(taddr0 + 256 + c0, u);
           tmem_ld_wait();
-          if constexpr (KIND == kGateUpSave) {
-            float2* o = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
+          float2* o = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              if (in_m && c0 + c < t.valid) *o = make_float2(__uint_as_float(g[c]), __uint_as_float(u[c]));
+          for (int c = 0; c < 16; ++c) {
+            const float gc = __uint_as_float(g[c]), uc = __uint_as_float(u[c]);
+            const float sg = sigmoid(gc), q = gc * sg;
+            g[c] = __float_as_uint(q * uc);
+            if constexpr (KIND == kGateUpSave) {
+              if (in_m && c0 + c < t.valid) *o = make_float2(uc * fmaf(q, 1.0f - sg, sg), q);
               o += ld;
             }
           }
 #pragma unroll
           for (int c = 0; c < 8; ++c)
-            act[i][c] = pack16(silu_mul(__uint_as_float(g[2 * c]), __uint_as_float(u[2 * c])),
-                               silu_mul(__uint_as_float(g[2 * c + 1]), __uint_as_float(u[2 * c + 1])), fp16);
+            act[i][c] = pack16(__uint_as_float(g[2 * c]), __uint_as_float(g[2 * c + 1]), fp16);
         }
         tc_fence_before();
         __syncwarp();
@@ -323,11 +362,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
         for (int i = 0; i < 4; ++i) {
           const int c0 = 16 * (group + 4 * i);
           if (c0 >= t.valid) continue;
-          store_cols(act[i], reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
+          store_cols<8>(act[i], reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
         }
       } else {
 #pragma unroll 1
         for (int acc = 0; acc < 2; ++acc) {
+          float2 pq[8];
+          auto load_saved = [&](float2* to, const Item& it, int ac, int c0) {
+            const int m = it.m0 + args.R * (2 * ac + (int)rank) + row;
+            const bool in = row < args.R && m < p.M;
+            const float2* sp = args.saved + (long long)(it.n0 + c0) * ld + m;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              to[c] = in && c0 + c < it.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
+              sp += ld;
+            }
+          };
+          if (KIND == kDact && args.S == 1) load_saved(pq, t, acc, 16 * group);
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
           if (!ok) break;
           tc_fence_after();
@@ -370,43 +421,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
                   w[c] = pack16(__uint_as_float(v[i][2 * c]), __uint_as_float(v[i][2 * c + 1]), fp16);
-                store_cols(w, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+                store_cols<8>(w, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
               }
             }
           } else {
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-              const int c0 = 16 * (group + 4 * i);
-              if (c0 >= t.valid) continue;
-              const long long at = (long long)(t.n0 + c0) * ld + m0;
-              float2 gu[16];
-              const float2* sp = args.saved + at + lane;
+            // units of 8 columns; the saved values of the next one are on their way while one is computed, those of
+            // the first since before the accumulator was waited for
 #pragma unroll
-              for (int c = 0; c < 16; ++c) {
-                gu[c] = in_m && c0 + c < t.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
-                sp += ld;
-              }
-              uint32_t v[16], wa[8], wg[8], wu[8];
-              tmem_ld16(taddr + c0, v);
+            for (int i = 0; i < 8; ++i) {
+              const int c0 = 16 * (group + 4 * (i >> 1)) + 8 * (i & 1);
+              if (c0 >= t.valid) continue;
+              const int c1 = 16 * (group + 4 * ((i + 1) >> 1)) + 8 * ((i + 1) & 1);
+              float2 next[8];
+              if (i < 7) load_saved(next, t, acc, c1);
+              uint32_t v[8], wg[4], wu[4];
+              tmem_ld8(taddr + c0, v);
               tmem_ld_wait();
 #pragma unroll
-              for (int c = 0; c < 8; ++c) {
-                float a2[2], g2[2], u2[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                  const float g = gu[2 * c + q].x, u = gu[2 * c + q].y, da = __uint_as_float(v[2 * c + q]);
-                  const float sg = sigmoid(g), sw = g * sg;
-                  a2[q] = silu_mul(g, u);  // the forward pass's bits
-                  g2[q] = da * u * fmaf(sw, 1.0f - sg, sg);
-                  u2[q] = da * sw;
-                }
-                wa[c] = pack16(a2[0], a2[1], fp16);
-                wg[c] = pack16(g2[0], g2[1], fp16);
-                wu[c] = pack16(u2[0], u2[1], fp16);
+              for (int c = 0; c < 4; ++c) {
+                const float d0 = __uint_as_float(v[2 * c]), d1 = __uint_as_float(v[2 * c + 1]);
+                wg[c] = pack16(d0 * pq[2 * c].x, d1 * pq[2 * c + 1].x, fp16);
+                wu[c] = pack16(d0 * pq[2 * c].y, d1 * pq[2 * c + 1].y, fp16);
               }
-              store_cols(wa, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
-              store_cols(wg, reinterpret_cast<uint16_t*>(args.dg) + at, ld, c0, t.valid, in_m, lane);
-              store_cols(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
+              const long long at = (long long)(t.n0 + c0) * ld + m0;
+              store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+              store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
+              if (i < 7) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) pq[c] = next[c];
+              }
             }
             tc_fence_before();
             __syncwarp();
@@ -424,9 +467,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
 // neighbouring m a thread.
 template <bool DACT>
 __global__ void __launch_bounds__(256) ffn_join_kernel(const float* planes, int S, long long n, const void* residual,
-                                                       const float2* saved, void* out, void* dg, void* du, int fp16) {
-  pdl_launch_dependents();
+                                                       const float2* saved, void* out, void* du, int fp16) {
   pdl_wait();
+  pdl_launch_dependents();  // behind the wait: the launch that follows may read the weights ahead
   const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= n) return;
   float4 v = ld_l2(reinterpret_cast<const float4*>(planes + i));
@@ -444,22 +487,10 @@ __global__ void __launch_bounds__(256) ffn_join_kernel(const float* planes, int 
         make_uint2(pack16(v.x, v.y, fp16), pack16(v.z, v.w, fp16));
   } else {
     const float4 s0 = ld_l2(reinterpret_cast<const float4*>(saved + i)), s1 = ld_l2(reinterpret_cast<const float4*>(saved + i) + 1);
-    const float g[4] = {s0.x, s0.z, s1.x, s1.z}, u[4] = {s0.y, s0.w, s1.y, s1.w}, da[4] = {v.x, v.y, v.z, v.w};
-    float a4[4], g4[4], u4[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float sg = sigmoid(g[q]), sw = g[q] * sg;
-      a4[q] = silu_mul(g[q], u[q]);
-      g4[q] = da[q] * u[q] * fmaf(sw, 1.0f - sg, sg);
-      u4[q] = da[q] * sw;
-    }
-    auto put = [&](void* o, const float* f) {
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(o) + i) =
-          make_uint2(pack16(f[0], f[1], fp16), pack16(f[2], f[3], fp16));
-    };
-    put(out, a4);
-    put(dg, g4);
-    put(du, u4);
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) =
+        make_uint2(pack16(v.x * s0.x, v.y * s0.z, fp16), pack16(v.z * s1.x, v.w * s1.z, fp16));
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(du) + i) =
+        make_uint2(pack16(v.x * s0.y, v.y * s0.w, fp16), pack16(v.z * s1.y, v.w * s1.w, fp16));
   }
 }
 
@@ -469,40 +500,52 @@ struct Plan {
   int R, n_tile, S, mt, nt;
 };
 
-// Tile and split of a launch of M x N outputs and KB k-blocks, by a model in SM cycles: an item's k-block takes what
-// bounds it, the tensor pipe (N / 2 cycles for each of 8 MMAs) or the bytes that a CTA draws from L2 (about 36 a
-// cycle with every SM drawing); an item has a fixed part and an epilogue; items are dealt to the pairs in rounds; a
-// split launch writes and reads planes.  Among equals the earlier, larger tile.
+// Tile and split of a launch of M x N outputs and KB k-blocks, by a model in SM cycles.  A k-block of an item takes
+// the largest of
+//   4.6 n_tile          the tensor pipe: eight MMAs of n_tile / 2 cycles, which the ring of stages keeps 88 % busy,
+//   bytes / 7600        what all running pairs draw from L2, 128 bytes for each row of A and column of B
+//   bytes / 3800        what they draw from HBM: rows of A that no other running item shares,
+//   bytes / 110         what a pair by itself can draw,
+//   4500 / stages       the latency of memory, for stages of few bytes
+// and an item a fixed part and an epilogue besides; items are dealt to the pairs in rounds, and in the last round
+// fewer pairs share the memory.  A split launch writes its planes and the join reads them.  Measured, gate/up launch
+// of 4096 tokens (h 4096, f 14336, R 128; cycles per k-block of an item with its epilogue's share, and TB/s from L2):
+// n_tile 256 1271, 8.4; 192 969, 11.0; 128 842, 11.4; 64 778, 12.3; 32 746, 12.2.  Rows that are no multiple of 8 leave
+// a swizzle atom in part empty and cost 18 % (R 98 against 112, n_tile 256).
 Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   const int unit = gate_up(kind) ? 2 : 4;
   Plan best = {};
   double best_cost = 1e300;
-  for (int cols = 256; cols >= 32; cols -= 32) {
+  for (int cols = 256; cols >= 16; cols -= 16) {
     const int nt = (N + cols - 1) / cols;
-    const int n_tile = ((N + nt - 1) / nt + 31) / 32 * 32;
+    const int n_tile = ((N + nt - 1) / nt + 15) / 16 * 16;
     if (n_tile != cols) continue;  // the same tiles with fewer columns come later
     for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4)); ++S) {
       const int kbs = (KB + S - 1) / S;
       if ((KB + kbs - 1) / kbs != S) continue;
       const int mt_min = (M + unit * kAccRows - 1) / (unit * kAccRows);
       const int least = (mt_min * nt * S + pairs - 1) / pairs;
-      for (int rounds = least; rounds <= least + 1; ++rounds) {
-        int R, mt;
-        if (a_mn(kind)) {
-          R = rounds == least ? 128 : 64;
-        } else {
-          const int most = rounds * pairs / (nt * S);
-          if (most < 1) continue;
-          R = ((M + unit * most - 1) / (unit * most) + 1) / 2 * 2;
-          if (R < 8) R = 8;
-          if (R > kAccRows) R = kAccRows;
+      for (int fill = 0; fill < 2; ++fill) {  // whole tiles, or as many rows as fill the rounds
+        int R = kAccRows;
+        if (fill) {
+          if (a_mn(kind)) {
+            R = 64;
+          } else {
+            const int most = least * pairs / (nt * S);
+            R = ((M + unit * most - 1) / (unit * most) + 7) / 8 * 8;
+          }
+          if (R >= kAccRows) continue;
         }
-        mt = (M + unit * R - 1) / (unit * R);
-        const int r = (mt * nt * S + pairs - 1) / pairs;
-        const double bytes = 2.0 * ((R + 7) / 8 * 8) * 128 + n_tile / 2 * 128.0;
-        const double kb = std::max(4.0 * n_tile, bytes / 36.0);
-        double cost = r * (kbs * kb + 2000.0 + 10.0 * n_tile);
-        if (S > 1) cost += 3000.0 + (double)S * N * M * 8 / (148 * 20.0);
+        const int mt = (M + unit * R - 1) / (unit * R);
+        const int items = mt * nt * S, full = items / pairs, rest = items - full * pairs;
+        auto round = [&](int active) {
+          const double l2 = active * (4.0 * R + n_tile) * 128 / 7600.0;
+          const double hbm = active * 4.0 * R * 128 / (active < nt ? active : nt) / 3800.0;
+          const double own = std::max((4.0 * R + n_tile) * 128 / 110.0, 4500.0 / kMaxStages);
+          return kbs * std::max(std::max(4.6 * n_tile, own), std::max(l2, hbm)) + 1500.0 + (gate_up(kind) ? 16.0 : 6.0) * n_tile;
+        };
+        double cost = full * (full ? round(pairs) : 0.0) + (rest ? round(rest) : 0.0);
+        if (S > 1) cost += 4000.0 + (double)S * N * M * 8 / 7000.0;
         if (cost < best_cost) {
           best_cost = cost;
           best = {R, n_tile, S, mt, nt};
@@ -524,6 +567,7 @@ template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, int pairs
   const int tail = std::max(0, kAccRows * 128 - a.slot_a);
   a.stages = std::min(kMaxStages, (kSmemLimit - 1024 - tail) / a.stage);
   a.kbs = (a.KB + a.S - 1) / a.S;
+  a.stages = std::min(a.stages, std::max(2, a.kbs));
   int items = 0;
   for (int p = 0; p < a.np; ++p) items += a.p[p].mt * a.p[p].nt;
   items *= a.S;
@@ -557,9 +601,9 @@ cudaError_t launch_join(bool dact, const Args& a, cudaStream_t st) {
   const dim3 grid((unsigned)((n / 4 + 255) / 256));
   if (dact)
     return launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, (const void*)nullptr,
-                      (const float2*)a.saved, a.p[0].out, a.dg, a.du, a.fp16);
+                      (const float2*)a.saved, a.p[0].out, a.du, a.fp16);
   return launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, a.residual,
-                    (const float2*)nullptr, a.p[0].out, (void*)nullptr, (void*)nullptr, a.fp16);
+                    (const float2*)nullptr, a.p[0].out, (void*)nullptr, a.fp16);
 }
 
 Args args_of(const Plan& p, int M, int N, int KB, void* out, int dtype) {
@@ -585,6 +629,9 @@ Plan gu_plan(int T, int h, int f, int pairs) { return choose_plan(kGateUp, f, T,
 Plan down_plan(int T, int h, int f, int pairs) { return choose_plan(kPlain, h, T, kblocks(f), true, pairs); }
 Plan dact_plan(int T, int h, int f, int pairs) { return choose_plan(kDact, f, T, kblocks(h), true, pairs); }
 Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kDx, h, T, 2 * kblocks(f), true, pairs); }
+
+// the saved buffer: (p, q), then a
+size_t pq_bytes(int T, int f) { return round256((size_t)T * f * sizeof(float2)); }
 
 size_t plane_bytes(const Plan& p, int T, int M) { return p.S > 1 ? round256((size_t)p.S * T * M * sizeof(float)) : 0; }
 
@@ -633,7 +680,7 @@ extern "C" {
 
 size_t moe_ffn_saved_bytes(int T, int f) {
   if (T < 1 || T > kMaxOperatorTokens || f < 8 || f % 8 || f > (1 << 20)) return 0;
-  return (size_t)T * f * sizeof(float2);
+  return pq_bytes(T, f) + (size_t)T * f * 2;
 }
 
 size_t moe_ffn_forward_workspace(int T, int h, int f) {
@@ -644,7 +691,7 @@ size_t moe_ffn_forward_workspace(int T, int h, int f) {
 size_t moe_ffn_backward_workspace(int T, int h, int f) {
   if (T < 1 || check_block(T, h, f, MOE_BF16)) return 0;
   const int pairs = sm_count() / 2;
-  return 3 * round256((size_t)T * f * 2) +
+  return 2 * round256((size_t)T * f * 2) +
          std::max(plane_bytes(dact_plan(T, h, f, pairs), T, f), plane_bytes(dx_plan(T, h, f, pairs), T, h));
 }
 
@@ -657,7 +704,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   if (!aligned16(x) || !aligned16(W1) || !aligned16(W3) || !aligned16(W2) || !aligned16(residual) || !aligned16(y) ||
       !aligned16(saved) || !aligned16(workspace))
     return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
-  const size_t n = (size_t)T * h * 2, w = (size_t)h * f * 2, n_saved = (size_t)T * f * sizeof(float2);
+  const size_t n = (size_t)T * h * 2, w = (size_t)h * f * 2, n_saved = moe_ffn_saved_bytes(T, f);
   if (overlap(y, n, x, n) || overlap(y, n, W1, w) || overlap(y, n, W3, w) || overlap(y, n, W2, w) ||
       overlap(y, n, saved, n_saved) || (residual != y && overlap(y, n, residual, n)))
     return set_error(MOE_ERR_INVALID_ARG, "y overlaps another tensor (only the residual itself is allowed)");
@@ -668,7 +715,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int pairs = sm_count() / 2;
   char* ws = static_cast<char*>(workspace);
-  void* act = ws;
+  void* act = saved ? static_cast<char*>(saved) + pq_bytes(T, f) : ws;
   Plan p = gu_plan(T, h, f, pairs);
   Args a = args_of(p, f, T, kblocks(h), act, dtype);
   a.saved = static_cast<float2*>(saved);
@@ -680,6 +727,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   p = down_plan(T, h, f, pairs);
   a = args_of(p, h, T, kblocks(f), y, dtype);
   a.residual = residual;
+  a.early = 1;
   a.planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
   FFN_MAP(map_k(&maps.a[0], W2, f, h, p.R));
   FFN_MAP(map_k(&maps.b[0], act, f, T, p.n_tile / 2));
@@ -701,7 +749,7 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   void* outs[4] = {dW1, dW3, dW2, dx};
   const size_t out_bytes[4] = {w, w, w, n};
   const void* ins[6] = {dy, x, W1, W3, W2, saved};
-  const size_t in_bytes[6] = {n, n, w, w, w, (size_t)T * f * sizeof(float2)};
+  const size_t in_bytes[6] = {n, n, w, w, w, moe_ffn_saved_bytes(T, f)};
   for (int i = 0; i < 4; ++i) {
     for (int j = 0; j < 6; ++j)
       if (overlap(outs[i], out_bytes[i], ins[j], in_bytes[j]))
@@ -726,14 +774,14 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   const int pairs = sm_count() / 2;
   char* ws = static_cast<char*>(workspace);
   const size_t part = round256((size_t)T * f * 2);
-  void *act = ws, *dg = ws + part, *du = ws + 2 * part;
-  float* planes = reinterpret_cast<float*>(ws + 3 * part);
+  const void* act = static_cast<const char*>(saved) + pq_bytes(T, f);
+  void *dg = ws, *du = ws + part;
+  float* planes = reinterpret_cast<float*>(ws + 2 * part);
   Maps maps = {};
-  // da = dy W2, and a, dg, du
+  // da = dy W2, and dg, du
   Plan p = dact_plan(T, h, f, pairs);
-  Args a = args_of(p, f, T, kblocks(h), act, dtype);
+  Args a = args_of(p, f, T, kblocks(h), dg, dtype);
   a.saved = static_cast<float2*>(const_cast<void*>(saved));
-  a.dg = dg;
   a.du = du;
   a.planes = planes;
   FFN_MAP(map_mn(&maps.a[0], W2, f, h));
@@ -744,6 +792,7 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   p = dx_plan(T, h, f, pairs);
   a = args_of(p, h, T, 2 * kblocks(f), dx, dtype);
   a.segKB = kblocks(f);
+  a.early = 1;
   a.planes = planes;
   FFN_MAP(map_mn(&maps.a[0], W1, h, f));
   FFN_MAP(map_mn(&maps.a[1], W3, h, f));

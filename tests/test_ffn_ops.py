@@ -74,7 +74,8 @@ def test_refuses_bad_arguments_without_a_device(lib):
     assert bwd(ws=None) == -1 and bwd(n=100) == -1 and "workspace" in binding.last_error()
     assert bwd(dt=2) == -1 and bwd(h=12) == -2 and bwd(T=-1) == -1
     assert lib.moe_ffn_saved_bytes(0, 64) == 0 and lib.moe_ffn_saved_bytes(3, 60) == 0
-    assert lib.moe_ffn_saved_bytes(3, 64) == 3 * 64 * 8
+    assert lib.moe_ffn_saved_bytes(3, 64) == 3 * 64 * 8 + 3 * 64 * 2
+    assert lib.moe_ffn_saved_bytes(1, 8) == 256 + 16
     assert lib.moe_ffn_forward_workspace(0, 64, 64) == 0 and lib.moe_ffn_backward_workspace(3, 60, 64) == 0
 
 
@@ -91,8 +92,8 @@ def test_tiles_cover_every_output(lib, h, f):
                 R, n_tile, S, mt, nt, kb = list(out)
                 M = f if launch in (0, 2) else h
                 unit = 2 if launch == 0 else 4
-                assert 8 <= R <= 128 and R % (64 if launch >= 2 else 2) == 0, (T, launch, list(out))
-                assert n_tile % 32 == 0 and 32 <= n_tile <= 256
+                assert 8 <= R <= 128 and R % (64 if launch >= 2 else 8) == 0, (T, launch, list(out))
+                assert n_tile % 16 == 0 and 16 <= n_tile <= 256
                 assert (mt - 1) * unit * R < M <= mt * unit * R and (nt - 1) * n_tile < T <= nt * n_tile
                 kbs = -(-kb // S)
                 assert 1 <= S <= 16 and (S - 1) * kbs < kb <= S * kbs
@@ -105,7 +106,7 @@ def test_tiles_cover_every_output(lib, h, f):
                 if S > 1:
                     ws = lib.moe_ffn_forward_workspace if launch == 1 else lib.moe_ffn_backward_workspace
                     if pairs == 74:  # without a device the library assumes 148 multiprocessors
-                        assert ws(T, h, f) >= T * f * 2 + S * T * M * 4
+                        assert ws(T, h, f) >= T * f * 2 * (1 if launch == 1 else 2) + S * T * M * 4
 
 
 def test_binding_refuses_host_tensors(lib):
@@ -113,7 +114,7 @@ def test_binding_refuses_host_tensors(lib):
     with pytest.raises(binding.MoeError):
         binding.ffn_forward(x, W, W, V)
     with pytest.raises(binding.MoeError):
-        binding.ffn_backward(x, x, W, W, V, torch.zeros((4, 8, 2)))
+        binding.ffn_backward(x, x, W, W, V, torch.zeros(lib.moe_ffn_saved_bytes(4, 8), dtype=torch.uint8))
 
 
 @gpu
@@ -207,10 +208,18 @@ def test_forward(T, h, f, dt):
     assert torch.equal(binding.ffn_forward(x, W1, W3, W2), y)  # a fixed order of the sums
     saved = binding.ffn_saved(T, f, DEV)
     assert torch.equal(binding.ffn_forward(x, W1, W3, W2, saved=saved), y)
-    for k, W in ((0, W1), (1, W3)):
-        want = x.double() @ W.double().T
-        size = x.double().abs() @ W.double().abs().T
-        assert bool(((saved[:, :, k].double() - want).abs() <= h * E23 * size).all())
+    # what is saved: u silu'(g) and silu(g) in fp32, then a
+    g, u = x.double() @ W1.double().T, x.double() @ W3.double().T
+    eg, eu = (h * E23 * (x.double().abs() @ W.double().abs().T) for W in (W1, W3))
+    sig = torch.sigmoid(g)
+    p, q = u * (sig + g * sig * (1 - sig)), g * sig
+    kept = saved[: T * f * 8].view(torch.float32).view(T, f, 2).double()
+    assert bool(((kept[:, :, 0] - p).abs() <= 1.1 * eu + u.abs() * 0.5 * eg + 0.5 * eu * eg + 2.0 ** -18 * u.abs()).all())
+    assert bool(((kept[:, :, 1] - q).abs() <= 1.1 * eg + 2.0 ** -18 * q.abs() + 1e-37).all())
+    a = saved[-(-T * f * 8 // 256) * 256:].view(dt).view(T, f).double()
+    half = torch.finfo(dt).eps / 2
+    assert bool(((a - q * u).abs() <= half * (q * u).abs() * 1.01 + 1.1 * eg * u.abs() + q.abs() * eu + 1.1 * eg * eu + 2.0 ** -17 * a.abs()
+                 + torch.finfo(dt).smallest_normal * half * 2).all())
     assert binding.operators_status(DEV) == 0
 
 
@@ -317,7 +326,7 @@ def test_nothing_is_written_behind_the_outputs(T):
         return whole, whole[: shape[0]]
 
     wy, y = room(T, h)
-    ws, saved = room(T, f, 2, dtype=torch.float32)
+    ws, saved = room(binding.load_library().moe_ffn_saved_bytes(T, f), dtype=torch.uint8)
     binding.ffn_forward(x, W1, W3, W2, y=y, saved=saved)
     rooms = [room(T, h), room(f, h), room(f, h), room(h, f)]
     binding.ffn_backward(dy, x, W1, W3, W2, saved, *[r[1] for r in rooms])
