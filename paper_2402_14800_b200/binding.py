@@ -8,6 +8,7 @@ library is missing or a call fails, a ``MoeError`` is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from math import comb
 
@@ -367,13 +368,12 @@ def _operand(name, t, dtype, shape, index):
     """Address of a contiguous tensor of this type and shape on this device; None for None."""
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index
-            and t.is_contiguous()):
-        raise MoeError(-1, "%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s" % (
-            name, dtype, tuple(shape), index,
-            "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride()) if isinstance(t, torch.Tensor)
-            else type(t).__name__))
-    return t.data_ptr()
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise MoeError(-1, "%s must be a contiguous %s tensor of shape %s on cuda:%d, got %s" % (
+        name, dtype, tuple(shape), index,
+        "%s %s on %s, strides %s" % (t.dtype, tuple(t.shape), t.device, t.stride()) if isinstance(t, torch.Tensor)
+        else type(t).__name__))
 
 
 def _on_device_of(x, dims, stream, body, *args):
@@ -481,6 +481,14 @@ def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
     return dx, dgain
 
 
+@functools.lru_cache(maxsize=256)
+def _ffn_bytes(T: int, h: int, f: int, index: int):
+    """(saved, forward workspace, backward workspace) in bytes on this device, which is current."""
+    lib = load_library()
+    return (int(lib.moe_ffn_saved_bytes(T, f)), int(lib.moe_ffn_forward_workspace(T, h, f)),
+            int(lib.moe_ffn_backward_workspace(T, h, f)))
+
+
 def ffn_saved(T: int, f: int, device) -> torch.Tensor:
     """A buffer for what ``ffn_forward`` saves for ``ffn_backward`` (``moe_ffn_saved_bytes``)."""
     return torch.empty((int(load_library().moe_ffn_saved_bytes(T, f)),), dtype=torch.uint8, device=device)
@@ -506,14 +514,13 @@ def _ffn_forward(index, st, x, W1, W3, W2, residual, y, saved):
     xp = _operand("x", x, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
     w2, rp = _operand("W2", W2, dt, (h, f), index), _operand("residual", residual, dt, shape, index)
-    lib = load_library()
-    sp = _operand("saved", saved, torch.uint8, (lib.moe_ffn_saved_bytes(T, f),), index)
+    n_saved, n, _ = _ffn_bytes(T, h, f, index)
+    sp = _operand("saved", saved, torch.uint8, (n_saved,), index)
     if y is None:
         y = torch.empty_like(x)
     yp = _operand("y", y, dt, shape, index)
-    n = lib.moe_ffn_forward_workspace(T, h, f)
     ws = x.new_empty((n,), dtype=torch.uint8)
-    _check(lib.moe_ffn_forward(xp, w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
+    _check(load_library().moe_ffn_forward(xp, w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
     return y
 
 
@@ -528,15 +535,14 @@ def _ffn_backward(index, st, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2):
     dt, shape = x.dtype, x.shape
     dp, xp = _operand("d_y", d_y, dt, shape, index), _operand("x", x, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
-    lib = load_library()
-    w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.uint8, (lib.moe_ffn_saved_bytes(T, f),), index)
+    n_saved, _, n = _ffn_bytes(T, h, f, index)
+    w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.uint8, (n_saved,), index)
     dx = torch.empty_like(x) if dx is None else dx
     dW1 = torch.empty_like(W1) if dW1 is None else dW1
     dW3 = torch.empty_like(W3) if dW3 is None else dW3
     dW2 = torch.empty_like(W2) if dW2 is None else dW2
-    n = lib.moe_ffn_backward_workspace(T, h, f)
     ws = x.new_empty((n,), dtype=torch.uint8)
-    _check(lib.moe_ffn_backward(dp, xp, w1, w3, w2, sp, T, h, f, DTYPES[dt], _operand("dx", dx, dt, shape, index),
+    _check(load_library().moe_ffn_backward(dp, xp, w1, w3, w2, sp, T, h, f, DTYPES[dt], _operand("dx", dx, dt, shape, index),
                                 _operand("dW1", dW1, dt, (f, h), index), _operand("dW3", dW3, dt, (f, h), index),
                                 _operand("dW2", dW2, dt, (h, f), index), ws.data_ptr(), n, st))
     return dx, dW1, dW3, dW2

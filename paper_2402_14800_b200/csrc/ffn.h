@@ -1,0 +1,21 @@
+// Dense feed-forward block: what its two paths share (ffn_sm100.cu: tensor cores, ffn_few.cu: few tokens).
+#pragma once
+
+#include "operators.h"
+
+namespace moe {
+
+constexpr int kFfnFewTokens = 32;  // most tokens of the second
+
+// Whether a forward call that saves nothing runs the kernels for few tokens: their rows have to fit shared memory.
+bool ffn_few_fits(int tokens, int h, int f);
+// act [tokens][f] is scratch of the tensors' type
+cudaError_t launch_ffn_few(const void* x, const void* W1, const void* W3, const void* W2, const void* residual, int tokens,
+                            int h, int f, int dtype, void* act, void* y, cudaStream_t st);
+
+#ifdef __CUDACC__
+// 1 / (1 + exp(-g)) by the fast exponential and reciprocal: a few units of the last place, 0 for g below -87
+__device__ __forceinline__ float ffn_sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
+#endif
+
+}  // namespace moe

@@ -34,8 +34,8 @@
 #include <algorithm>
 #include <atomic>
 
+#include "ffn.h"
 #include "moe_test_hooks.h"
-#include "operators.h"
 #include "sm100.h"
 
 namespace moe {
@@ -46,9 +46,18 @@ __device__ int g_status;  // set when a bounded wait of this file's kernels expi
 
 enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kDx, kDw };
 
-constexpr int kEpiWarps = 16;
-constexpr int kGemmThreads = 96 + 32 * kEpiWarps;
-constexpr int kSmemLimit = 230400;      // dynamic shared memory of a CTA, the barrier block lies beside it
+// Launches of at most 64 columns, or 128 with a contraction of at most 16 k-blocks, run a slim form of the kernel, half
+// an SM each in shared memory, registers and tensor memory: with few tokens what counts is the gap between two launches,
+// and the next launch's CTAs set up and fetch their first weights beside the last ones of this launch.  Forward pass in
+// us, full form / slim form, tokens 64 and 128: (h 512, f 1024) 18.6 / 16.3, 18.1 / 16.8; (2048, 4096) 31.7 / 29.8, 32.9 /
+// 33.9; (4096, 4096) 48.8 / 46.5, 50.6 / 63.9; (4096, 14336) 76.6 / 75.8, 78.9 / 90.9.
+template <bool SLIM> struct Form {
+  static constexpr int kEpiWarps = SLIM ? 4 : 16;
+  static constexpr int kThreads = 96 + 32 * kEpiWarps;
+  static constexpr int kAccCols = SLIM ? 128 : 256;            // columns of an accumulator, of which there are two
+  static constexpr int kChunks = kAccCols / 4 / kEpiWarps;     // chunks of 16 columns a warp reads of an accumulator
+  static constexpr int kSmem = SLIM ? 114688 : 230400;         // dynamic shared memory at most
+};
 constexpr int kAccRows = 128;           // rows of an accumulator in one CTA
 constexpr int kMaxStages = 8;           // size of the barrier block
 constexpr int kBandTiles = 16;          // n tiles that sweep the m tiles together
@@ -176,14 +185,14 @@ __device__ __forceinline__ void store_cols(const uint32_t* v, uint16_t* out, lon
   }
 }
 
-// 1 / (1 + exp(-g)) by the fast exponential and reciprocal: a few units of the last place, 0 for g below -87
-__device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
-
-template <int KIND>
-__global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
+template <int KIND, bool SLIM>
+__global__ void __launch_bounds__(Form<SLIM>::kThreads, SLIM ? 2 : 1)
+ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ Bars bars;
   constexpr bool AMN = a_mn(KIND), BMN = b_mn(KIND), GU = gate_up(KIND);
+  constexpr int kEpiWarps = Form<SLIM>::kEpiWarps, kAccCols = Form<SLIM>::kAccCols, kChunks = Form<SLIM>::kChunks;
+  constexpr int kStride = kEpiWarps / 4;  // of a warp's chunks
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();  // 0 = leader of the pair
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
 
   setup_barriers<kMaxStages>(bars, 2 * kEpiWarps, 2);
   if (warp == 1) {
-    tmem_alloc_pair(smem_u32(&bars.tmem_base), 512);
+    tmem_alloc_pair(smem_u32(&bars.tmem_base), 2 * kAccCols);
     tmem_relinquish_pair();
   }
   constexpr int kMapsA = KIND == kDw ? 3 : GU || KIND == kDx ? 2 : 1, kMapsB = KIND == kDw ? 3 : KIND == kDx ? 2 : 1;
@@ -275,7 +284,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
     // ---- MMA issuers of the leader, one warp per accumulator
     if (rank == 0) {
       const uint32_t acc = (uint32_t)warp - 1u;
-      const uint32_t d_tmem = tmem_base + 256u * acc;
+      const uint32_t d_tmem = tmem_base + (uint32_t)kAccCols * acc;
       const uint32_t tmem_full = smem_u32(&bars.tmem_full[acc]), tmem_empty = smem_u32(&bars.tmem_empty[acc]);
       const uint32_t idesc = idesc16(256, args.n_tile, args.fp16, AMN, BMN);
       constexpr uint32_t sa_k = AMN ? kStepMn : kStepK, sb_k = BMN ? kStepMn : kStepK;
@@ -307,7 +316,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
     }
   } else {
     pdl_wait();
-    // ---- epilogue: warp w reads tensor-memory lanes 32 (w % 4) .. + 31, and of the chunks of 16 columns every fourth
+    // ---- epilogue: warp w reads tensor-memory lanes 32 (w % 4) .. + 31, and of the chunks of 16 columns every kStride-th
     const int wq = warp & 3, group = (warp - 3) >> 2;
     const int row = 32 * wq + lane;  // row of this thread in its CTA's part of an accumulator
     const uint32_t empty0 = map_to_cta(smem_u32(&bars.tmem_empty[0]), 0);
@@ -327,20 +336,24 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
         tc_fence_after();
         const int m0 = t.m0 + args.R * (int)rank + 32 * wq;  // of lane 0
         const bool in_m = row < args.R && m0 + lane < p.M;
-        uint32_t act[4][8];
+        auto store_act = [&](const uint32_t* act, int c0) {  // R and M are even: both m of a lane's pair exist or neither
+          store_cols<8>(act, reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
+        };
+        // with rounds of items to come the accumulators go back to the MMAs before the stores; slim launches have one
+        uint32_t act[SLIM ? 1 : kChunks][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c0 = 16 * (group + 4 * i);
+        for (int i = 0; i < kChunks; ++i) {
+          const int c0 = 16 * (group + kStride * i);
           if (c0 >= t.valid) continue;
           uint32_t g[16], u[16];
           tmem_ld16(taddr0 + c0, g);
-          tmem_ld16(taddr0 + 256 + c0, u);
+          tmem_ld16(taddr0 + kAccCols + c0, u);
           tmem_ld_wait();
           float2* o = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
             const float gc = __uint_as_float(g[c]), uc = __uint_as_float(u[c]);
-            const float sg = sigmoid(gc), q = gc * sg;
+            const float sg = ffn_sigmoid(gc), q = gc * sg;
             g[c] = __float_as_uint(q * uc);
             if constexpr (KIND == kGateUpSave) {
               if (in_m && c0 + c < t.valid) *o = make_float2(uc * fmaf(q, 1.0f - sg, sg), q);
@@ -349,7 +362,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
           }
 #pragma unroll
           for (int c = 0; c < 8; ++c)
-            act[i][c] = pack16(__uint_as_float(g[2 * c]), __uint_as_float(g[2 * c + 1]), fp16);
+            act[SLIM ? 0 : i][c] = pack16(__uint_as_float(g[2 * c]), __uint_as_float(g[2 * c + 1]), fp16);
+          if (SLIM) store_act(act[0], c0);
         }
         tc_fence_before();
         __syncwarp();
@@ -357,47 +371,132 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
           mbar_arrive_cluster(empty0);
           mbar_arrive_cluster(empty1);
         }
-        // R and M are even, so both m of a lane's pair exist or neither
+        if (!SLIM) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c0 = 16 * (group + 4 * i);
-          if (c0 >= t.valid) continue;
-          store_cols<8>(act[i], reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
+          for (int i = 0; i < kChunks; ++i) {
+            const int c0 = 16 * (group + kStride * i);
+            if (c0 < t.valid) store_act(act[SLIM ? 0 : i], c0);
+          }
         }
       } else {
+        if constexpr (!SLIM && KIND != kDact) {
+          // The usual case: both accumulators are read, rounded and handed back before the first store, so that the
+          // next item's MMAs run beside the stores.
+          if (KIND == kDw || (args.S == 1 && !(KIND == kPlain && args.residual))) {
+            uint32_t w[2][kChunks][8];
+#pragma unroll
+            for (int acc = 0; acc < 2; ++acc) {
+              ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int i = 0; i < kChunks; ++i) {
+                uint32_t v[16];
+                tmem_ld16(taddr0 + kAccCols * acc + 16 * (group + kStride * i), v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                  w[acc][i][c] = pack16(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]), fp16);
+              }
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+            }
+            if (!ok) break;
+#pragma unroll
+            for (int acc = 0; acc < 2; ++acc) {
+              const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
+              const bool in_m = row < args.R && m0 + lane < p.M;
+#pragma unroll
+              for (int i = 0; i < kChunks; ++i) {
+                const int c0 = 16 * (group + kStride * i);
+                if (c0 < t.valid)
+                  store_cols<8>(w[acc][i], reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0,
+                                t.valid, in_m, lane);
+              }
+            }
+            continue;
+          }
+        }
+        if constexpr (KIND == kDact) {
+          if (args.S == 1) {
+            // Units of 8 columns; the saved values of the next one are on their way while one is computed, those of the
+            // first since before the accumulator was waited for.  (Fetching them to L2 during the MMAs was 20 % slower at
+            // 2048 tokens, h 4096, f 14336: they were evicted again, and 649 MB came from HBM where 436 MB do now.  To L2
+            // a few units ahead made no difference; two units ahead in registers spilled.)
+#pragma unroll 1
+            for (int acc = 0; acc < 2; ++acc) {
+              const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
+              const bool in_m = row < args.R && m0 + lane < p.M;
+              float2 pq[8];
+              auto load_saved = [&](float2* to, int c0) {
+                const float2* sp = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                  to[c] = in_m && c0 + c < t.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
+                  sp += ld;
+                }
+              };
+              load_saved(pq, 16 * group);
+              ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int i = 0; i < 2 * kChunks; ++i) {
+                const int c0 = 16 * (group + kStride * (i >> 1)) + 8 * (i & 1);
+                if (c0 >= t.valid) continue;
+                float2 next[8];
+                if (i + 1 < 2 * kChunks) load_saved(next, 16 * (group + kStride * ((i + 1) >> 1)) + 8 * ((i + 1) & 1));
+                uint32_t v[8], wg[4], wu[4];
+                tmem_ld8(taddr0 + kAccCols * acc + c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  const float d0 = __uint_as_float(v[2 * c]), d1 = __uint_as_float(v[2 * c + 1]);
+                  wg[c] = pack16(d0 * pq[2 * c].x, d1 * pq[2 * c + 1].x, fp16);
+                  wu[c] = pack16(d0 * pq[2 * c].y, d1 * pq[2 * c + 1].y, fp16);
+                }
+                const long long at = (long long)(t.n0 + c0) * ld + m0;
+                store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+                store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
+                if (i + 1 < 2 * kChunks) {
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) pq[c] = next[c];
+                }
+              }
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+            }
+            if (!ok) break;
+            continue;
+          }
+        }
+        if constexpr (KIND != kDw) {
 #pragma unroll 1
         for (int acc = 0; acc < 2; ++acc) {
-          float2 pq[8];
-          auto load_saved = [&](float2* to, const Item& it, int ac, int c0) {
-            const int m = it.m0 + args.R * (2 * ac + (int)rank) + row;
-            const bool in = row < args.R && m < p.M;
-            const float2* sp = args.saved + (long long)(it.n0 + c0) * ld + m;
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              to[c] = in && c0 + c < it.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
-              sp += ld;
-            }
-          };
-          if (KIND == kDact && args.S == 1) load_saved(pq, t, acc, 16 * group);
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t taddr = taddr0 + 256 * acc;
+          const uint32_t taddr = taddr0 + kAccCols * acc;
           const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
           const bool in_m = row < args.R && m0 + lane < p.M;
-          if (KIND != kDact || args.S > 1) {
-            // everything this warp wants of the accumulator goes to registers, and the accumulator back to the
-            // MMAs, before the stores
+          // everything this warp wants of the accumulator goes to registers, and the accumulator back to the
+          // MMAs, before the stores
+#pragma unroll 1
+          for (int j = 0; j < kChunks; j += 4) {
             uint32_t v[4][16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_ld16(taddr + 16 * (group + 4 * i), v[i]);
+            for (int i = 0; i < 4; ++i) tmem_ld16(taddr + 16 * (group + kStride * (j + i)), v[i]);
             tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+            if (j + 4 >= kChunks) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int c0 = 16 * (group + 4 * i);
+              const int c0 = 16 * (group + kStride * (j + i));
               if (c0 >= t.valid) continue;
               const long long at = (long long)(t.n0 + c0) * ld + m0;
               if (KIND != kDw && args.S > 1) {
@@ -424,43 +523,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ffn_gemm_kernel(const __grid_
                 store_cols<8>(w, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
               }
             }
-          } else {
-            // units of 8 columns; the saved values of the next one are on their way while one is computed, those of
-            // the first since before the accumulator was waited for
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int c0 = 16 * (group + 4 * (i >> 1)) + 8 * (i & 1);
-              if (c0 >= t.valid) continue;
-              const int c1 = 16 * (group + 4 * ((i + 1) >> 1)) + 8 * ((i + 1) & 1);
-              float2 next[8];
-              if (i < 7) load_saved(next, t, acc, c1);
-              uint32_t v[8], wg[4], wu[4];
-              tmem_ld8(taddr + c0, v);
-              tmem_ld_wait();
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const float d0 = __uint_as_float(v[2 * c]), d1 = __uint_as_float(v[2 * c + 1]);
-                wg[c] = pack16(d0 * pq[2 * c].x, d1 * pq[2 * c + 1].x, fp16);
-                wu[c] = pack16(d0 * pq[2 * c].y, d1 * pq[2 * c + 1].y, fp16);
-              }
-              const long long at = (long long)(t.n0 + c0) * ld + m0;
-              store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
-              store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
-              if (i < 7) {
-#pragma unroll
-                for (int c = 0; c < 8; ++c) pq[c] = next[c];
-              }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
           }
+        }
         }
       }
     }
   }
 
-  teardown_pair(bars, tmem_base, 512, issued, ns, rank, &g_status);
+  teardown_pair(bars, tmem_base, 2 * kAccCols, issued, ns, rank, &g_status);
 }
 
 // Sum of the S planes of a split launch in their order, and what the epilogue would have done with it: four
@@ -498,7 +568,26 @@ __global__ void __launch_bounds__(256) ffn_join_kernel(const float* planes, int 
 
 struct Plan {
   int R, n_tile, S, mt, nt;
+  bool slim;
 };
+
+// Pipeline of a tile: bytes of an accumulator's rows of A and of a stage, and the stages that fit.
+struct Ring {
+  int slot_a, stage, tail, stages;
+};
+
+
+Ring ring_of(int kind, int R, int n_tile, bool slim) {
+  Ring r;
+  r.slot_a = a_mn(kind) ? (R + 63) / 64 * (int)kMnBoxBytes : (R + 7) / 8 * 1024;
+  const int half = n_tile / 2;
+  r.stage = 2 * r.slot_a + (b_mn(kind) ? (half + 63) / 64 * (int)kMnBoxBytes : half * 128);
+  // an MMA reads 128 rows of A whatever was loaded: up to 16 KB behind the last slot
+  r.tail = std::max(0, kAccRows * 128 - r.slot_a);
+  const int smem = slim ? Form<true>::kSmem : Form<false>::kSmem;
+  r.stages = std::min(kMaxStages, (smem - 1024 - r.tail) / r.stage);
+  return r;
+}
 
 // Tile and split of a launch of M x N outputs and KB k-blocks, by a model in SM cycles.  A k-block of an item takes
 // the largest of
@@ -512,18 +601,19 @@ struct Plan {
 // of 4096 tokens (h 4096, f 14336, R 128; cycles per k-block of an item with its epilogue's share, and TB/s from L2):
 // n_tile 256 1271, 8.4; 192 969, 11.0; 128 842, 11.4; 64 778, 12.3; 32 746, 12.2.  Rows that are no multiple of 8 leave
 // a swizzle atom in part empty and cost 18 % (R 98 against 112, n_tile 256).
-Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
+Plan search_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   const int unit = gate_up(kind) ? 2 : 4;
   Plan best = {};
   double best_cost = 1e300;
-  for (int cols = 256; cols >= 16; cols -= 16) {
+  const bool slim = N <= 64 || (N <= Form<true>::kAccCols && KB <= 16);
+  const int mt_min = (M + unit * kAccRows - 1) / (unit * kAccRows);
+  for (int cols = slim ? Form<true>::kAccCols : 256; cols >= 16; cols -= 16) {
     const int nt = (N + cols - 1) / cols;
     const int n_tile = ((N + nt - 1) / nt + 15) / 16 * 16;
     if (n_tile != cols) continue;  // the same tiles with fewer columns come later
-    for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4)); ++S) {
+    for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4 && (S - 1) * nt * mt_min < 2 * pairs)); ++S) {
       const int kbs = (KB + S - 1) / S;
       if ((KB + kbs - 1) / kbs != S) continue;
-      const int mt_min = (M + unit * kAccRows - 1) / (unit * kAccRows);
       const int least = (mt_min * nt * S + pairs - 1) / pairs;
       for (int fill = 0; fill < 2; ++fill) {  // whole tiles, or as many rows as fill the rounds
         int R = kAccRows;
@@ -538,17 +628,18 @@ Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
         }
         const int mt = (M + unit * R - 1) / (unit * R);
         const int items = mt * nt * S, full = items / pairs, rest = items - full * pairs;
+        const int stages = ring_of(kind, R, n_tile, slim).stages;
         auto round = [&](int active) {
           const double l2 = active * (4.0 * R + n_tile) * 128 / 7600.0;
           const double hbm = active * 4.0 * R * 128 / (active < nt ? active : nt) / 3800.0;
-          const double own = std::max((4.0 * R + n_tile) * 128 / 110.0, 4500.0 / kMaxStages);
+          const double own = std::max((4.0 * R + n_tile) * 128 / 110.0, 4500.0 / stages);
           return kbs * std::max(std::max(4.6 * n_tile, own), std::max(l2, hbm)) + 1500.0 + (gate_up(kind) ? 16.0 : 6.0) * n_tile;
         };
         double cost = full * (full ? round(pairs) : 0.0) + (rest ? round(rest) : 0.0);
-        if (S > 1) cost += 4000.0 + (double)S * N * M * 8 / 7000.0;
+        if (S > 1) cost += 6000.0 + (double)S * N * M * 8 / 7000.0;
         if (cost < best_cost) {
           best_cost = cost;
-          best = {R, n_tile, S, mt, nt};
+          best = {R, n_tile, S, mt, nt, slim};
         }
       }
     }
@@ -556,18 +647,29 @@ Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   return best;
 }
 
+// The same, remembered for the sizes that this thread asked about last: a search takes 1 to 8 us of the host, and a call
+// needs each plan two or three times.
+Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
+  struct Known {
+    int kind, M, N, KB, pairs;
+    Plan plan;
+  };
+  static thread_local Known known[16] = {};
+  const unsigned hash = (unsigned)M * 0x9e3779b1u ^ (unsigned)N * 0x85ebca6bu ^ (unsigned)KB * 0xc2b2ae35u ^ (unsigned)kind * 0x27d4eb2fu;
+  Known& k = known[(hash >> 16) & 15u];
+  if (k.kind != kind || k.M != M || k.N != N || k.KB != KB || k.pairs != pairs)
+    k = {kind, M, N, KB, pairs, search_plan(kind, M, N, KB, may_split, pairs)};
+  return k.plan;
+}
+
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
-  a.slot_a = a_mn(KIND) ? (a.R + 63) / 64 * (int)kMnBoxBytes : (a.R + 7) / 8 * 1024;
-  const int half = a.n_tile / 2;
-  const int slot_b = b_mn(KIND) ? (half + 63) / 64 * (int)kMnBoxBytes : half * 128;
-  a.stage = 2 * a.slot_a + slot_b;
-  // an MMA reads 128 rows of A (and whole boxes of columns) whatever was loaded: up to 32 KB behind the last slot
-  const int tail = std::max(0, kAccRows * 128 - a.slot_a);
-  a.stages = std::min(kMaxStages, (kSmemLimit - 1024 - tail) / a.stage);
+template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
+  const Ring ring = ring_of(KIND, a.R, a.n_tile, SLIM);
+  a.slot_a = ring.slot_a;
+  a.stage = ring.stage;
   a.kbs = (a.KB + a.S - 1) / a.S;
-  a.stages = std::min(a.stages, std::max(2, a.kbs));
+  a.stages = std::min(ring.stages, std::max(2, a.kbs));
   int items = 0;
   for (int p = 0; p < a.np; ++p) items += a.p[p].mt * a.p[p].nt;
   items *= a.S;
@@ -576,14 +678,14 @@ template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, int pairs
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !(set.load() >> dev & 1)) {
-    e = cudaFuncSetAttribute(ffn_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+    e = cudaFuncSetAttribute(ffn_gemm_kernel<KIND, SLIM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Form<SLIM>::kSmem);
     if (e != cudaSuccess) return e;
     if (dev < 64) set.fetch_or(1ull << dev);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * std::min(items, pairs));
-  cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = 1024 + (size_t)a.stages * a.stage + tail;
+  cfg.blockDim = dim3(Form<SLIM>::kThreads);
+  cfg.dynamicSmemBytes = 1024 + (size_t)a.stages * a.stage + ring.tail;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -593,7 +695,13 @@ template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, int pairs
   attr[1].val.programmaticStreamSerializationAllowed = g_pdl_enabled ? 1 : 0;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<KIND>, maps, a);
+  return cudaLaunchKernelEx(&cfg, ffn_gemm_kernel<KIND, SLIM>, maps, a);
+}
+
+template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, bool slim, int pairs, cudaStream_t st) {
+  if constexpr (KIND != kDw)
+    if (slim) return launch_form<KIND, true>(maps, a, pairs, st);
+  return launch_form<KIND, false>(maps, a, pairs, st);
 }
 
 cudaError_t launch_join(bool dact, const Args& a, cudaStream_t st) {
@@ -716,6 +824,10 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   const int pairs = sm_count() / 2;
   char* ws = static_cast<char*>(workspace);
   void* act = saved ? static_cast<char*>(saved) + pq_bytes(T, f) : ws;
+  if (!saved && ffn_few_fits(T, h, f)) {
+    FFN_TRY("launch for few tokens", launch_ffn_few(x, W1, W3, W2, residual, T, h, f, dtype, act, y, st));
+    return MOE_OK;
+  }
   Plan p = gu_plan(T, h, f, pairs);
   Args a = args_of(p, f, T, kblocks(h), act, dtype);
   a.saved = static_cast<float2*>(saved);
@@ -723,7 +835,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   FFN_MAP(map_k(&maps.a[0], W1, h, f, p.R));
   FFN_MAP(map_k(&maps.a[1], W3, h, f, p.R));
   FFN_MAP(map_k(&maps.b[0], x, h, T, p.n_tile / 2));
-  FFN_TRY("gate/up launch", saved ? launch_gemm<kGateUpSave>(maps, a, pairs, st) : launch_gemm<kGateUp>(maps, a, pairs, st));
+  FFN_TRY("gate/up launch", saved ? launch_gemm<kGateUpSave>(maps, a, p.slim, pairs, st) : launch_gemm<kGateUp>(maps, a, p.slim, pairs, st));
   p = down_plan(T, h, f, pairs);
   a = args_of(p, h, T, kblocks(f), y, dtype);
   a.residual = residual;
@@ -731,7 +843,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   a.planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
   FFN_MAP(map_k(&maps.a[0], W2, f, h, p.R));
   FFN_MAP(map_k(&maps.b[0], act, f, T, p.n_tile / 2));
-  FFN_TRY("down launch", launch_gemm<kPlain>(maps, a, pairs, st));
+  FFN_TRY("down launch", launch_gemm<kPlain>(maps, a, p.slim, pairs, st));
   if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
   return MOE_OK;
 }
@@ -786,7 +898,7 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   a.planes = planes;
   FFN_MAP(map_mn(&maps.a[0], W2, f, h));
   FFN_MAP(map_k(&maps.b[0], dy, h, T, p.n_tile / 2));
-  FFN_TRY("da launch", launch_gemm<kDact>(maps, a, pairs, st));
+  FFN_TRY("da launch", launch_gemm<kDact>(maps, a, p.slim, pairs, st));
   if (p.S > 1) FFN_TRY("join launch", launch_join(true, a, st));
   // dx = dg W1 + du W3
   p = dx_plan(T, h, f, pairs);
@@ -798,10 +910,10 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   FFN_MAP(map_mn(&maps.a[1], W3, h, f));
   FFN_MAP(map_k(&maps.b[0], dg, f, T, p.n_tile / 2));
   FFN_MAP(map_k(&maps.b[1], du, f, T, p.n_tile / 2));
-  FFN_TRY("dx launch", launch_gemm<kDx>(maps, a, pairs, st));
+  FFN_TRY("dx launch", launch_gemm<kDx>(maps, a, p.slim, pairs, st));
   if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
   // dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
-  a = args_of({kAccRows, 256, 1, 0, 0}, 0, 0, kblocks(T), nullptr, dtype);
+  a = args_of({kAccRows, 256, 1, 0, 0, false}, 0, 0, kblocks(T), nullptr, dtype);
   a.np = 3;
   const int rows = 4 * a.R;
   a.p[0] = {h, f, (h + rows - 1) / rows, (f + a.n_tile - 1) / a.n_tile, dW1};
@@ -813,7 +925,7 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   FFN_MAP(map_mn(&maps.b[1], du, f, T));
   FFN_MAP(map_mn(&maps.b[2], dy, h, T));
   maps.a[1] = maps.a[0];
-  FFN_TRY("weight gradients launch", launch_gemm<kDw>(maps, a, pairs, st));
+  FFN_TRY("weight gradients launch", launch_gemm<kDw>(maps, a, false, pairs, st));
   return MOE_OK;
 }
 

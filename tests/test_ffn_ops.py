@@ -93,7 +93,7 @@ def test_tiles_cover_every_output(lib, h, f):
                 M = f if launch in (0, 2) else h
                 unit = 2 if launch == 0 else 4
                 assert 8 <= R <= 128 and R % (64 if launch >= 2 else 8) == 0, (T, launch, list(out))
-                assert n_tile % 16 == 0 and 16 <= n_tile <= 256
+                assert n_tile % 16 == 0 and 16 <= n_tile <= (128 if T <= 128 else 256)
                 assert (mt - 1) * unit * R < M <= mt * unit * R and (nt - 1) * n_tile < T <= nt * n_tile
                 kbs = -(-kb // S)
                 assert 1 <= S <= 16 and (S - 1) * kbs < kb <= S * kbs
@@ -102,7 +102,7 @@ def test_tiles_cover_every_output(lib, h, f):
                 # a stage of the pipeline fits, and so does what an MMA reads behind the last one
                 slot = -(-R // 64) * 8192 if launch >= 2 else -(-R // 8) * 1024
                 stage, tail = 2 * slot + n_tile * 64, max(0, 16384 - slot)
-                assert 1024 + tail + 2 * stage <= 230400
+                assert 1024 + tail + 2 * stage <= (114688 if T <= 128 else 230400)
                 if S > 1:
                     ws = lib.moe_ffn_forward_workspace if launch == 1 else lib.moe_ffn_backward_workspace
                     if pairs == 74:  # without a device the library assumes 148 multiprocessors
@@ -194,11 +194,14 @@ def check(got, want, dt, name):
 
 SIZES = [(1, 8, 8), (3, 64, 8), (2, 8, 200), (1, 128, 448), (100, 128, 448), (31, 72, 136), (33, 520, 264), (128, 1000, 2728),
          (256, 256, 512), (257, 264, 520), (300, 2048, 4096), (611, 2040, 5464), (1025, 512, 1032), (2500, 136, 72)]
+FEW = [(2, 4096, 14336), (3, 4096, 14336), (4, 40, 24), (5, 128, 448), (7, 4096, 14336), (8, 2040, 5464), (9, 1000, 2728),
+       (16, 2048, 4096), (24, 264, 1032), (32, 1024, 2048), (33, 640, 1032), (50, 72, 1528), (64, 512, 1024), (64, 1528, 8),
+       (40, 8, 1528), (12, 4096, 72), (6, 72, 14336)]
 
 
 @gpu
 @pytest.mark.parametrize("dt", list(TYPES))
-@pytest.mark.parametrize("T,h,f", SIZES + [(1, 4096, 14336), (17, 4096, 14336), (128, 4096, 14336), (200, 4096, 14336),
+@pytest.mark.parametrize("T,h,f", SIZES + FEW + [(1, 4096, 14336), (17, 4096, 14336), (128, 4096, 14336), (200, 4096, 14336),
                                            (1000, 4096, 14336)])
 def test_forward(T, h, f, dt):
     dt = TYPES[dt]
@@ -207,7 +210,10 @@ def test_forward(T, h, f, dt):
     check(y, reference(x, W1, W3, W2)["y"], dt, "y")
     assert torch.equal(binding.ffn_forward(x, W1, W3, W2), y)  # a fixed order of the sums
     saved = binding.ffn_saved(T, f, DEV)
-    assert torch.equal(binding.ffn_forward(x, W1, W3, W2, saved=saved), y)
+    y2 = binding.ffn_forward(x, W1, W3, W2, saved=saved)
+    check(y2, reference(x, W1, W3, W2)["y"], dt, "y")
+    if T > 32:  # few tokens have kernels of their own where nothing is saved
+        assert torch.equal(y2, y)
     # what is saved: u silu'(g) and silu(g) in fp32, then a
     g, u = x.double() @ W1.double().T, x.double() @ W3.double().T
     eg, eu = (h * E23 * (x.double().abs() @ W.double().abs().T) for W in (W1, W3))
@@ -271,7 +277,7 @@ def test_backward_is_the_slope_of_forward():
 
 
 @gpu
-@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("T", [1, 2, 6, 40, 300])
 @pytest.mark.parametrize("dt", list(TYPES))
 def test_residual_is_added_before_the_rounding(T, dt):
     dt = TYPES[dt]
@@ -298,16 +304,18 @@ def test_no_tokens():
 
 
 @gpu
-@pytest.mark.parametrize("T", [5, 40, 300])
+@pytest.mark.parametrize("T", [3, 5, 40, 300])
 def test_a_bad_token_spoils_only_its_own_rows(T):
     h, f = 520, 1032
     x, W1, W3, W2, dy = make(T, h, f, torch.bfloat16, seed=5)
     saved, saved_bad = binding.ffn_saved(T, f, DEV), binding.ffn_saved(T, f, DEV)
-    y = binding.ffn_forward(x, W1, W3, W2, saved=saved)
+    y = binding.ffn_forward(x, W1, W3, W2)
+    binding.ffn_forward(x, W1, W3, W2, saved=saved)
     dx, *_ = binding.ffn_backward(dy, x, W1, W3, W2, saved)
     bad = x.clone()
     bad[T // 2, 3], bad[T - 1, 0] = float("nan"), float("inf")
-    y_bad = binding.ffn_forward(bad, W1, W3, W2, saved=saved_bad)
+    y_bad = binding.ffn_forward(bad, W1, W3, W2)
+    binding.ffn_forward(bad, W1, W3, W2, saved=saved_bad)
     dx_bad, *_ = binding.ffn_backward(dy, bad, W1, W3, W2, saved_bad)
     keep = [t for t in range(T) if t not in (T // 2, T - 1)]
     assert torch.equal(y_bad[keep], y[keep]) and torch.equal(dx_bad[keep], dx[keep])
@@ -315,7 +323,7 @@ def test_a_bad_token_spoils_only_its_own_rows(T):
 
 
 @gpu
-@pytest.mark.parametrize("T", [1, 37, 300])
+@pytest.mark.parametrize("T", [1, 2, 5, 37, 300])
 def test_nothing_is_written_behind_the_outputs(T):
     h, f = 136, 264
     x, W1, W3, W2, dy = make(T, h, f, torch.bfloat16, seed=6)
@@ -340,7 +348,8 @@ def test_nothing_is_written_behind_the_outputs(T):
     st = torch.cuda.current_stream().cuda_stream
     assert lib.moe_ffn_forward(x.data_ptr(), W1.data_ptr(), W3.data_ptr(), W2.data_ptr(), None, T, h, f, 0, y2.data_ptr(), None,
                                buf.data_ptr(), n, st) == 0
-    assert torch.equal(y2, y) and bool((buf[n:] == 9).all())
+    check(y2, reference(x, W1, W3, W2)["y"], torch.bfloat16, "y")
+    assert bool((buf[n:] == 9).all())
     n = lib.moe_ffn_backward_workspace(T, h, f)
     buf = torch.full((n + 512,), 9, dtype=torch.uint8, device=DEV)
     outs = [torch.empty_like(t) for t in (x, W1, W3, W2)]
@@ -386,9 +395,12 @@ def test_two_streams_at_once_and_graphs(T):
     for a, b in got:
         assert all(torch.equal(p, q) for p, q in zip(a, want[0])) and all(torch.equal(p, q) for p, q in zip(b, want[1]))
     side = torch.cuda.Stream()
-    y = binding.ffn_forward(*sets[0][:4], stream=side)
+    saved = binding.ffn_saved(T, f, DEV)
+    side.wait_stream(torch.cuda.current_stream())
+    y = binding.ffn_forward(*sets[0][:4], saved=saved, stream=side)
+    alone = binding.ffn_forward(*sets[0][:4], stream=side)
     side.synchronize()
-    assert torch.equal(y, want[0][0])
+    assert torch.equal(y, want[0][0]) and torch.equal(alone, binding.ffn_forward(*sets[0][:4]))
     # two graphs, each with its own workspaces, replayed beside each other
     graphs, outs = [], []
     for s in sets:
