@@ -44,7 +44,7 @@ namespace {
 
 __device__ int g_status;  // set when a bounded wait of this file's kernels expired
 
-enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kDx, kDw };
+enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kGrads };
 
 // Launches of at most 64 columns, or 128 with a contraction of at most 16 k-blocks, run a slim form of the kernel, half
 // an SM each in shared memory, registers and tensor memory: with few tokens what counts is the gap between two launches,
@@ -62,24 +62,26 @@ constexpr int kAccRows = 128;           // rows of an accumulator in one CTA
 constexpr int kMaxStages = 8;           // size of the barrier block
 constexpr int kBandTiles = 16;          // n tiles that sweep the m tiles together
 
-// A operand contiguous in m (W2 of da, W1 and W3 of dx, x and a of the weights' gradients); B contiguous in n
-constexpr __host__ __device__ bool a_mn(int kind) { return kind == kDact || kind == kDx || kind == kDw; }
-constexpr __host__ __device__ bool b_mn(int kind) { return kind == kDw; }
+// A operand contiguous in m (W2 of da, W1 and W3 of dx, x and a of the weights' gradients)
+constexpr __host__ __device__ bool a_mn(int kind) { return kind == kDact || kind == kGrads; }
 constexpr __host__ __device__ bool gate_up(int kind) { return kind == kGateUp || kind == kGateUpSave; }
 
 struct Problem {
-  int M, N;    // m and n range
-  int mt, nt;  // tiles
-  void* out;   // [N][M]
+  int M, N;       // m and n range
+  int mt, nt;     // tiles
+  void* out;      // [N][M]
+  int KB, segKB;  // k-blocks of 64; of one segment (dx: two segments, else segKB = KB)
+  int S, kbs;     // k-splits, k-blocks of each
+  int R, n_tile;  // rows of A a CTA and accumulator loads, columns of an item
+  int a0, b0;     // tensor maps of the first segment
+  int bmn;        // B contiguous in n (weights' gradients)
 };
 
 struct Args {
-  Problem p[3];
-  int np;             // problems of the launch (the three weight gradients), else 1
-  int KB, segKB;      // k-blocks of 64; of one segment (dx: two segments, else segKB = KB)
-  int S, kbs;         // k-splits, k-blocks of each
-  int R, n_tile;      // rows of A a CTA and accumulator loads, columns of an item
-  int stages, slot_a, stage;  // pipeline stages, bytes of an accumulator's A tile, of a stage
+  Problem p[4];               // kGrads: dx, dW1, dW3, dW2
+  int np;
+  int first, skip;            // kGrads: the dx items, one a pair, count as `skip` rounds of the others
+  int stages, slot_a, stage, tail;  // pipeline stages, bytes of an accumulator's A tile, of a stage, behind the last one
   int fp16;
   const void* residual;       // kPlain
   float2* saved;              // [N][M] (p, q): written by kGateUpSave, read by kDact
@@ -89,7 +91,7 @@ struct Args {
 };
 
 struct Maps {
-  CUtensorMap a[3], b[3];
+  CUtensorMap a[5], b[5];
 };
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int fp16) {
@@ -121,6 +123,17 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* v) {
                : "r"(taddr)
                : "memory");
 }
+// copies of 16 bytes through L2 to shared memory (bytes = 0: zeros), in groups; all groups but the newest
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait_but_one() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+__device__ __forceinline__ float2 load8_shared(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
 __device__ __forceinline__ void prefetch_tensor_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
@@ -140,19 +153,28 @@ struct Item {
   int valid;                       // columns that exist
 };
 
+// The k-th item of a pair, past the last one when there is none.  Items are dealt in rounds; where dx shares a launch
+// with the weights' gradients the pairs that got one of its long items join the rounds of short ones late.
+template <int KIND> __device__ __forceinline__ int item_of(const Args& a, int k, int pair, int n_pairs) {
+  if (KIND != kGrads || a.first == 0) return pair + k * n_pairs;
+  const int rest = n_pairs - a.first;
+  if (pair < a.first) return k == 0 ? pair : a.first + a.skip * rest + (k - 1) * n_pairs + pair;
+  return a.first + (k < a.skip ? k * rest + pair - a.first : a.skip * rest + (k - a.skip) * n_pairs + pair);
+}
+
 // Items of a problem: k-split -> band of at most kBandTiles n tiles -> m tile -> n tile, so that the items in
 // flight share few tiles of either operand in L2.
 template <int KIND> __device__ __forceinline__ Item decode_item(const Args& a, int item) {
   Item t;
   t.prob = 0;
-  if (KIND == kDw) {
-    while (t.prob + 1 < a.np && item >= a.p[t.prob].mt * a.p[t.prob].nt) {
-      item -= a.p[t.prob].mt * a.p[t.prob].nt;
+  if (KIND == kGrads) {
+    while (t.prob + 1 < a.np && item >= a.p[t.prob].mt * a.p[t.prob].nt * a.p[t.prob].S) {
+      item -= a.p[t.prob].mt * a.p[t.prob].nt * a.p[t.prob].S;
       ++t.prob;
     }
   }
   const Problem& p = a.p[t.prob];
-  t.ks = KIND == kDw || gate_up(KIND) ? 0 : item / (p.mt * p.nt);
+  t.ks = gate_up(KIND) ? 0 : item / (p.mt * p.nt);
   item -= t.ks * p.mt * p.nt;
   const int bands = (p.nt + kBandTiles - 1) / kBandTiles;
   const int per_band = (p.nt + bands - 1) / bands;
@@ -160,11 +182,11 @@ template <int KIND> __device__ __forceinline__ Item decode_item(const Args& a, i
   const int rem = item - band * per_band * p.mt;
   const int band_tiles = min(per_band, p.nt - band * per_band);
   const int m = rem / band_tiles;
-  t.m0 = m * (gate_up(KIND) ? 2 : 4) * a.R;
-  t.n0 = (band * per_band + rem - m * band_tiles) * a.n_tile;
-  t.valid = min(a.n_tile, p.N - t.n0);
-  t.kb0 = t.ks * a.kbs;
-  t.kb1 = min(a.KB, t.kb0 + a.kbs);
+  t.m0 = m * (gate_up(KIND) ? 2 : 4) * p.R;
+  t.n0 = (band * per_band + rem - m * band_tiles) * p.n_tile;
+  t.valid = min(p.n_tile, p.N - t.n0);
+  t.kb0 = t.ks * p.kbs;
+  t.kb1 = min(p.KB, t.kb0 + p.kbs);
   return t;
 }
 
@@ -190,7 +212,7 @@ __global__ void __launch_bounds__(Form<SLIM>::kThreads, SLIM ? 2 : 1)
 ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
   extern __shared__ uint8_t smem_raw[];
   __shared__ Bars bars;
-  constexpr bool AMN = a_mn(KIND), BMN = b_mn(KIND), GU = gate_up(KIND);
+  constexpr bool AMN = a_mn(KIND), GU = gate_up(KIND);
   constexpr int kEpiWarps = Form<SLIM>::kEpiWarps, kAccCols = Form<SLIM>::kAccCols, kChunks = Form<SLIM>::kChunks;
   constexpr int kStride = kEpiWarps / 4;  // of a warp's chunks
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -203,7 +225,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
     tmem_alloc_pair(smem_u32(&bars.tmem_base), 2 * kAccCols);
     tmem_relinquish_pair();
   }
-  constexpr int kMapsA = KIND == kDw ? 3 : GU || KIND == kDx ? 2 : 1, kMapsB = KIND == kDw ? 3 : KIND == kDx ? 2 : 1;
+  constexpr int kMapsA = KIND == kGrads ? 5 : GU ? 2 : 1, kMapsB = KIND == kGrads ? 5 : 1;
   if (warp == 0 && lane < kMapsA) prefetch_tensor_map(&maps.a[lane]);
   if (warp == 0 && lane >= 8 && lane < 8 + kMapsB) prefetch_tensor_map(&maps.b[lane - 8]);
   __syncwarp();
@@ -214,41 +236,52 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
   volatile int* abort_flag = &bars.abort_flag;
 
   const uint32_t ns = (uint32_t)args.stages, stage_bytes = (uint32_t)args.stage, slot_a = (uint32_t)args.slot_a;
-  const int half = args.n_tile >> 1;  // a multiple of 8
   int n_items = 0;
-  for (int p = 0; p < (KIND == kDw ? args.np : 1); ++p) n_items += args.p[p].mt * args.p[p].nt;
-  if (KIND != kDw && !GU) n_items *= args.S;
+  for (int i = 0; i < (KIND == kGrads ? args.np : 1); ++i) n_items += args.p[i].mt * args.p[i].nt * args.p[i].S;
   uint32_t issued = 0;
 
   if (warp == 0) {
     // ---- TMA producer of this CTA's rows of A and its half of the columns; the bytes of both CTAs are counted on
     // the leader's barrier
-    const uint32_t a_bytes = AMN ? (uint32_t)((args.R + 63) >> 6) * kMnBoxBytes : (uint32_t)args.R * 128u;
-    const uint32_t b_bytes = BMN ? (uint32_t)((half + 63) >> 6) * kMnBoxBytes : (uint32_t)half * 128u;
-    const uint32_t bytes = 2u * (2u * a_bytes + b_bytes);
     uint32_t s = 0, ph = 0;
     bool ok = true;
     auto load_a = [&](const Item& t, int kb, uint32_t stage) {  // and what the stage's barrier expects
+      const Problem& p = args.p[t.prob];
+      const int half = p.n_tile >> 1;  // a multiple of 8
+      const uint32_t a_bytes = AMN ? (uint32_t)((p.R + 63) >> 6) * kMnBoxBytes : (uint32_t)p.R * 128u;
+      const uint32_t b_bytes = KIND == kGrads && p.bmn ? (uint32_t)((half + 63) >> 6) * kMnBoxBytes : (uint32_t)half * 128u;
       const uint32_t full = map_to_cta(smem_u32(&bars.full[stage]), 0), sa = smem_base + stage * stage_bytes;
-      if (rank == 0) mbar_expect_tx(smem_u32(&bars.full[stage]), bytes);
-      const int seg = KIND == kDx && kb >= args.segKB ? 1 : 0;
-      const int k0 = (kb - seg * args.segKB) * BK, row0 = t.m0 + args.R * (int)rank;
+      if (rank == 0) mbar_expect_tx(smem_u32(&bars.full[stage]), 2u * (2u * a_bytes + b_bytes));
+      const int seg = KIND == kGrads && kb >= p.segKB ? 1 : 0;
+      const int k0 = (kb - seg * p.segKB) * BK, row0 = t.m0 + p.R * (int)rank;
 #pragma unroll
       for (int acc = 0; acc < 2; ++acc) {
-        const CUtensorMap* map = &maps.a[GU ? acc : KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
-        const int row = GU ? row0 : row0 + 2 * args.R * acc;
+        const CUtensorMap* map = &maps.a[GU ? acc : p.a0 + seg];
+        const int row = GU ? row0 : row0 + 2 * p.R * acc;
         if (AMN) {
-          for (int j = 0; j < args.R; j += 64) tma_load_2d_pair(sa + acc * slot_a + j * 128, map, row + j, k0, full);
+          for (int j = 0; j < p.R; j += 64) tma_load_2d_pair(sa + acc * slot_a + j * 128, map, row + j, k0, full);
         } else {
           tma_load_2d_pair(sa + acc * slot_a, map, k0, row, full);
         }
+      }
+    };
+    auto load_b = [&](const Item& t, int kb, uint32_t stage) {
+      const Problem& p = args.p[t.prob];
+      const int half = p.n_tile >> 1, col0 = t.n0 + half * (int)rank;
+      const uint32_t full = map_to_cta(smem_u32(&bars.full[stage]), 0), sb = smem_base + stage * stage_bytes + 2 * slot_a;
+      const int seg = KIND == kGrads && kb >= p.segKB ? 1 : 0, k0 = (kb - seg * p.segKB) * BK;
+      const CUtensorMap* map = &maps.b[p.b0 + seg];
+      if (KIND == kGrads && p.bmn) {
+        for (int j = 0; j < half; j += 64) tma_load_2d_pair(sb + j * 128, map, col0 + j, k0, full);
+      } else {
+        tma_load_2d_pair(sb, map, k0, col0, full);
       }
     };
     // The launch before this one let it start after its own wait (below), so everything older than that launch is
     // complete, the weights among it: the first ring of stages of A may come before the wait.
     uint32_t ahead = 0;
     if (args.early && pair < n_items) {
-      const Item t = decode_item<KIND>(args, pair);
+      const Item t = decode_item<KIND>(args, item_of<KIND>(args, 0, pair, n_pairs));
       ahead = min(ns, (uint32_t)(t.kb1 - t.kb0));
       if (lane == 0)
         for (uint32_t i = 0; i < ahead; ++i) load_a(t, t.kb0 + (int)i, i);
@@ -256,24 +289,14 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
     }
     pdl_wait();
     pdl_launch_dependents();
-    for (int item = pair; item < n_items && ok; item += n_pairs) {
+    for (int k = 0, item; ok && (item = item_of<KIND>(args, k, pair, n_pairs)) < n_items; ++k) {
       const Item t = decode_item<KIND>(args, item);
-      const int col0 = t.n0 + half * (int)rank;
       for (int kb = t.kb0; kb < t.kb1; ++kb, ++issued) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.empty[s]), ph ^ 1u, abort_flag));
         if (!ok) break;
         if (lane == 0) {
-          const uint32_t full = map_to_cta(smem_u32(&bars.full[s]), 0);
-          const uint32_t sa = smem_base + s * stage_bytes;
-          const int seg = KIND == kDx && kb >= args.segKB ? 1 : 0;
-          const int k0 = (kb - seg * args.segKB) * BK;
           if (issued >= ahead) load_a(t, kb, s);
-          const CUtensorMap* map = &maps.b[KIND == kDx ? seg : KIND == kDw ? t.prob : 0];
-          if (BMN) {
-            for (int j = 0; j < half; j += 64) tma_load_2d_pair(sa + 2 * slot_a + j * 128, map, col0 + j, k0, full);
-          } else {
-            tma_load_2d_pair(sa + 2 * slot_a, map, k0, col0, full);
-          }
+          load_b(t, kb, s);
         }
         if (++s == ns) { s = 0; ph ^= 1u; }
         __syncwarp();
@@ -286,12 +309,14 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
       const uint32_t acc = (uint32_t)warp - 1u;
       const uint32_t d_tmem = tmem_base + (uint32_t)kAccCols * acc;
       const uint32_t tmem_full = smem_u32(&bars.tmem_full[acc]), tmem_empty = smem_u32(&bars.tmem_empty[acc]);
-      const uint32_t idesc = idesc16(256, args.n_tile, args.fp16, AMN, BMN);
-      constexpr uint32_t sa_k = AMN ? kStepMn : kStepK, sb_k = BMN ? kStepMn : kStepK;
+      constexpr uint32_t sa_k = AMN ? kStepMn : kStepK;
       uint32_t s = 0, ph = 0, nu = 0;  // nu: items so far
       bool ok = true;
-      for (int item = pair; item < n_items && ok; item += n_pairs, ++nu) {
+      for (int item; ok && (item = item_of<KIND>(args, (int)nu, pair, n_pairs)) < n_items; ++nu) {
         const Item t = decode_item<KIND>(args, item);
+        const bool bmn = KIND == kGrads && args.p[t.prob].bmn;
+        const uint32_t idesc = idesc16(256, args.p[t.prob].n_tile, args.fp16, AMN, bmn);
+        const uint32_t sb_k = bmn ? kStepMn : kStepK;
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           bool ready = mbar_wait(smem_u32(&bars.full[s]), ph, abort_flag);
           if (kb == t.kb0) ready = ready && mbar_wait(tmem_empty, (nu & 1u) ^ 1u, abort_flag);
@@ -301,7 +326,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
           if (lane == 0) {
             const uint32_t sa = smem_base + s * stage_bytes + acc * slot_a, sb = smem_base + s * stage_bytes + 2 * slot_a;
             const uint64_t adesc = AMN ? smem_desc_mn128(sa) : smem_desc_k128(sa);
-            const uint64_t bdesc = BMN ? smem_desc_mn128(sb) : smem_desc_k128(sb);
+            const uint64_t bdesc = bmn ? smem_desc_mn128(sb) : smem_desc_k128(sb);
             umma_bf16_pair(d_tmem, adesc, bdesc, idesc, kb > t.kb0 ? 1u : 0u);
             umma_bf16_pair(d_tmem, adesc + sa_k, bdesc + sb_k, idesc, 1u);
             umma_bf16_pair(d_tmem, adesc + 2 * sa_k, bdesc + 2 * sb_k, idesc, 1u);
@@ -325,17 +350,18 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
     const int fp16 = args.fp16;
     uint32_t nu = 0;
     bool ok = true;
-    for (int item = pair; item < n_items && ok; item += n_pairs, ++nu) {
+    for (int item; ok && (item = item_of<KIND>(args, (int)nu, pair, n_pairs)) < n_items; ++nu) {
       const Item t = decode_item<KIND>(args, item);
       const Problem& p = args.p[t.prob];
       const long long ld = p.M;
+      const int R = p.R;
       if constexpr (GU) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[0]), nu & 1u, abort_flag) &&
                                          mbar_wait(smem_u32(&bars.tmem_full[1]), nu & 1u, abort_flag));
         if (!ok) break;
         tc_fence_after();
-        const int m0 = t.m0 + args.R * (int)rank + 32 * wq;  // of lane 0
-        const bool in_m = row < args.R && m0 + lane < p.M;
+        const int m0 = t.m0 + R * (int)rank + 32 * wq;  // of lane 0
+        const bool in_m = row < R && m0 + lane < p.M;
         auto store_act = [&](const uint32_t* act, int c0) {  // R and M are even: both m of a lane's pair exist or neither
           store_cols<8>(act, reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
         };
@@ -382,7 +408,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
         if constexpr (!SLIM && KIND != kDact) {
           // The usual case: both accumulators are read, rounded and handed back before the first store, so that the
           // next item's MMAs run beside the stores.
-          if (KIND == kDw || (args.S == 1 && !(KIND == kPlain && args.residual))) {
+          if (p.S == 1 && !(KIND == kPlain && args.residual)) {
             uint32_t w[2][kChunks][8];
 #pragma unroll
             for (int acc = 0; acc < 2; ++acc) {
@@ -405,8 +431,8 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
             if (!ok) break;
 #pragma unroll
             for (int acc = 0; acc < 2; ++acc) {
-              const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
-              const bool in_m = row < args.R && m0 + lane < p.M;
+              const int m0 = t.m0 + R * (2 * acc + (int)rank) + 32 * wq;
+              const bool in_m = row < R && m0 + lane < p.M;
 #pragma unroll
               for (int i = 0; i < kChunks; ++i) {
                 const int c0 = 16 * (group + kStride * i);
@@ -419,68 +445,87 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
           }
         }
         if constexpr (KIND == kDact) {
-          if (args.S == 1) {
-            // Units of 8 columns; the saved values of the next one are on their way while one is computed, those of the
-            // first since before the accumulator was waited for.  (Fetching them to L2 during the MMAs was 20 % slower at
-            // 2048 tokens, h 4096, f 14336: they were evicted again, and 649 MB came from HBM where 436 MB do now.  To L2
-            // a few units ahead made no difference; two units ahead in registers spilled.)
+          if (p.S == 1) {
+            // Units of 8 columns, accumulator 0 and then 1.  What this epilogue waits for is the saved values: 235 MB at
+            // 2048 tokens (h 4096, f 14336), most of them from HBM, where 32 KB an SM in flight (8 columns a thread in
+            // registers) left the tensor cores idle for 40 % of the launch.  So a warp copies its values of two units ahead
+            // to shared memory, since before the accumulators are complete: of each two columns the even lanes one and
+            // the odd lanes the other, for two neighbouring rows (16 bytes).
+            // (Three stages of operands are as fast as four here.  Fetching all of it to L2 during the MMAs was 20 %
+            // slower: it was evicted again, and 649 MB came from HBM instead of 436.)
+            const uint32_t mine = smem_base + ns * stage_bytes + args.tail + ((warp - 3) * 32 + lane) * 8;
+            const int odd = lane & 1;
+            constexpr uint32_t kCol = kEpiWarps * 32 * 8;  // bytes of a column
+            int units = 0;  // of an accumulator
+            while (units < 2 * kChunks && 16 * (group + kStride * (units >> 1)) + 8 * (units & 1) < t.valid) ++units;
+            auto col_of = [&](int u) { return 16 * (group + kStride * (u >> 1)) + 8 * (u & 1); };
+            auto copy_unit = [&](int u) {
+              const int acc = u >= units, c0 = col_of(u - acc * units);
+              const int m = t.m0 + R * (2 * acc + (int)rank) + row - odd;  // even, and so are R and M
+              const bool in_m = row < R && m < p.M;
+              const float2* sp = args.saved + (long long)(t.n0 + c0 + odd) * ld + m;
+#pragma unroll
+              for (int c = 0; c < 8; c += 2) {
+                const bool in = in_m && c0 + c + odd < t.valid;
+                copy16_async(mine - 8 * odd + (8 * (u & 1) + c + odd) * kCol, in ? sp : args.saved, in ? 16 : 0);
+                sp += 2 * ld;
+              }
+            };
+            if (units) copy_unit(0);
+            copy_commit();
+            if (units) copy_unit(1);
+            copy_commit();
 #pragma unroll 1
-            for (int acc = 0; acc < 2; ++acc) {
-              const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
-              const bool in_m = row < args.R && m0 + lane < p.M;
-              float2 pq[8];
-              auto load_saved = [&](float2* to, int c0) {
-                const float2* sp = args.saved + (long long)(t.n0 + c0) * ld + m0 + lane;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                  to[c] = in_m && c0 + c < t.valid ? __ldcg(sp) : make_float2(0.f, 0.f);
-                  sp += ld;
-                }
-              };
-              load_saved(pq, 16 * group);
-              ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
-              if (!ok) break;
-              tc_fence_after();
-#pragma unroll
-              for (int i = 0; i < 2 * kChunks; ++i) {
-                const int c0 = 16 * (group + kStride * (i >> 1)) + 8 * (i & 1);
-                if (c0 >= t.valid) continue;
-                float2 next[8];
-                if (i + 1 < 2 * kChunks) load_saved(next, 16 * (group + kStride * ((i + 1) >> 1)) + 8 * ((i + 1) & 1));
-                uint32_t v[8], wg[4], wu[4];
+            for (int u = 0; u < max(2 * units, 2); ++u) {
+              const int acc = units ? u >= units : u, i = u - acc * units;
+              if (i == 0 || !units) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+              }
+              uint32_t v[8], wg[4], wu[4];
+              const int c0 = units ? col_of(i) : 0;
+              if (units) {
+                copy_wait_but_one();
+                __syncwarp();  // the neighbours' copies too
                 tmem_ld8(taddr0 + kAccCols * acc + c0, v);
                 tmem_ld_wait();
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  const float d0 = __uint_as_float(v[2 * c]), d1 = __uint_as_float(v[2 * c + 1]);
-                  wg[c] = pack16(d0 * pq[2 * c].x, d1 * pq[2 * c + 1].x, fp16);
-                  wu[c] = pack16(d0 * pq[2 * c].y, d1 * pq[2 * c + 1].y, fp16);
-                }
-                const long long at = (long long)(t.n0 + c0) * ld + m0;
-                store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
-                store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
-                if (i + 1 < 2 * kChunks) {
-#pragma unroll
-                  for (int c = 0; c < 8; ++c) pq[c] = next[c];
-                }
               }
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+              if (!units || i == units - 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(acc ? empty1 : empty0);
+              }
+              if (!units) continue;
+#pragma unroll
+              for (int c = 0; c < 4; ++c) {
+                const float2 a = load8_shared(mine + (8 * (u & 1) + 2 * c) * kCol);
+                const float2 b = load8_shared(mine + (8 * (u & 1) + 2 * c + 1) * kCol);
+                const float d0 = __uint_as_float(v[2 * c]), d1 = __uint_as_float(v[2 * c + 1]);
+                wg[c] = pack16(d0 * a.x, d1 * b.x, fp16);
+                wu[c] = pack16(d0 * a.y, d1 * b.y, fp16);
+              }
+              __syncwarp();  // all lanes have read what is written over
+              if (u + 2 < 2 * units) copy_unit(u + 2);
+              copy_commit();  // an empty group keeps the count
+              const int m0 = t.m0 + R * (2 * acc + (int)rank) + 32 * wq;
+              const bool in_m = row < R && m0 + lane < p.M;
+              const long long at = (long long)(t.n0 + c0) * ld + m0;
+              store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
+              store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
             }
             if (!ok) break;
             continue;
           }
         }
-        if constexpr (KIND != kDw) {
 #pragma unroll 1
         for (int acc = 0; acc < 2; ++acc) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.tmem_full[acc]), nu & 1u, abort_flag));
           if (!ok) break;
           tc_fence_after();
           const uint32_t taddr = taddr0 + kAccCols * acc;
-          const int m0 = t.m0 + args.R * (2 * acc + (int)rank) + 32 * wq;
-          const bool in_m = row < args.R && m0 + lane < p.M;
+          const int m0 = t.m0 + R * (2 * acc + (int)rank) + 32 * wq;
+          const bool in_m = row < R && m0 + lane < p.M;
           // everything this warp wants of the accumulator goes to registers, and the accumulator back to the
           // MMAs, before the stores
 #pragma unroll 1
@@ -499,7 +544,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
               const int c0 = 16 * (group + kStride * (j + i));
               if (c0 >= t.valid) continue;
               const long long at = (long long)(t.n0 + c0) * ld + m0;
-              if (KIND != kDw && args.S > 1) {
+              if (p.S > 1) {
                 float* o = args.planes + (long long)t.ks * p.N * ld + at + lane;
 #pragma unroll
                 for (int c = 0; c < 16; ++c) {
@@ -524,7 +569,6 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
               }
             }
           }
-        }
         }
       }
     }
@@ -577,15 +621,22 @@ struct Ring {
 };
 
 
+// Shared memory of the epilogue of the da launch: two units of 8 columns, 8 bytes a value.
+int saved_bytes(int kind, bool slim) { return kind == kDact ? 2 * 8 * 8 * 32 * (slim ? Form<true>::kEpiWarps : Form<false>::kEpiWarps) : 0; }
+
 Ring ring_of(int kind, int R, int n_tile, bool slim) {
   Ring r;
-  r.slot_a = a_mn(kind) ? (R + 63) / 64 * (int)kMnBoxBytes : (R + 7) / 8 * 1024;
-  const int half = n_tile / 2;
-  r.stage = 2 * r.slot_a + (b_mn(kind) ? (half + 63) / 64 * (int)kMnBoxBytes : half * 128);
+  if (kind == kGrads) {  // what the weights' gradients need, which is the most
+    r.slot_a = kAccRows / 64 * (int)kMnBoxBytes;
+    r.stage = 2 * r.slot_a + Form<false>::kAccCols / (slim ? 4 : 2) / 64 * (int)kMnBoxBytes;
+  } else {
+    r.slot_a = a_mn(kind) ? (R + 63) / 64 * (int)kMnBoxBytes : (R + 7) / 8 * 1024;
+    r.stage = 2 * r.slot_a + n_tile / 2 * 128;
+  }
   // an MMA reads 128 rows of A whatever was loaded: up to 16 KB behind the last slot
   r.tail = std::max(0, kAccRows * 128 - r.slot_a);
   const int smem = slim ? Form<true>::kSmem : Form<false>::kSmem;
-  r.stages = std::min(kMaxStages, (smem - 1024 - r.tail) / r.stage);
+  r.stages = std::min(kMaxStages, (smem - 1024 - r.tail - saved_bytes(kind, slim)) / r.stage);
   return r;
 }
 
@@ -601,11 +652,16 @@ Ring ring_of(int kind, int R, int n_tile, bool slim) {
 // of 4096 tokens (h 4096, f 14336, R 128; cycles per k-block of an item with its epilogue's share, and TB/s from L2):
 // n_tile 256 1271, 8.4; 192 969, 11.0; 128 842, 11.4; 64 778, 12.3; 32 746, 12.2.  Rows that are no multiple of 8 leave
 // a swizzle atom in part empty and cost 18 % (R 98 against 112, n_tile 256).
+bool is_slim(int kind, int M, int N, int KB) {
+  if (kind == kGrads) return N <= Form<true>::kAccCols && (long long)M * KB * 32 <= (1 << 19);  // KB: of two segments
+  return N <= 64 || (N <= Form<true>::kAccCols && KB <= 16);
+}
+
 Plan search_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   const int unit = gate_up(kind) ? 2 : 4;
   Plan best = {};
   double best_cost = 1e300;
-  const bool slim = N <= 64 || (N <= Form<true>::kAccCols && KB <= 16);
+  const bool slim = is_slim(kind, M, N, KB);
   const int mt_min = (M + unit * kAccRows - 1) / (unit * kAccRows);
   for (int cols = slim ? Form<true>::kAccCols : 256; cols >= 16; cols -= 16) {
     const int nt = (N + cols - 1) / cols;
@@ -665,14 +721,26 @@ Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
-  const Ring ring = ring_of(KIND, a.R, a.n_tile, SLIM);
+  const Ring ring = ring_of(KIND, a.p[0].R, a.p[0].n_tile, SLIM);
   a.slot_a = ring.slot_a;
   a.stage = ring.stage;
-  a.kbs = (a.KB + a.S - 1) / a.S;
-  a.stages = std::min(ring.stages, std::max(2, a.kbs));
-  int items = 0;
-  for (int p = 0; p < a.np; ++p) items += a.p[p].mt * a.p[p].nt;
-  items *= a.S;
+  a.tail = ring.tail;
+  int items = 0, kbs = 2;
+  for (int i = 0; i < a.np; ++i) {
+    Problem& p = a.p[i];
+    p.kbs = (p.KB + p.S - 1) / p.S;
+    kbs = std::max(kbs, p.kbs);
+    items += p.mt * p.nt * p.S;
+  }
+  a.stages = std::min(ring.stages, kbs);
+  if (KIND == kGrads) {
+    // an item of dx against one of the weights' gradients, in cycles: the tensor pipe, or what a pair draws of weights
+    // (600 a k-block) and stores (9000 an item)
+    const Problem &x = a.p[0], &w = a.p[1];
+    const int n = x.mt * x.nt * x.S, grid = std::min(items, pairs);
+    a.first = n < grid ? n : 0;
+    a.skip = a.first ? (int)(x.kbs * std::max(4.6 * x.n_tile, 600.0) / std::max(4.6 * w.n_tile * w.kbs + 4000.0, 9000.0)) : 0;
+  }
   static std::atomic<unsigned long long> set{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -685,7 +753,7 @@ template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * std::min(items, pairs));
   cfg.blockDim = dim3(Form<SLIM>::kThreads);
-  cfg.dynamicSmemBytes = 1024 + (size_t)a.stages * a.stage + ring.tail;
+  cfg.dynamicSmemBytes = 1024 + (size_t)a.stages * a.stage + ring.tail + saved_bytes(KIND, SLIM);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -699,31 +767,37 @@ template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a
 }
 
 template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, bool slim, int pairs, cudaStream_t st) {
-  if constexpr (KIND != kDw)
-    if (slim) return launch_form<KIND, true>(maps, a, pairs, st);
+  if (slim) return launch_form<KIND, true>(maps, a, pairs, st);
   return launch_form<KIND, false>(maps, a, pairs, st);
 }
 
 cudaError_t launch_join(bool dact, const Args& a, cudaStream_t st) {
-  const long long n = (long long)a.p[0].M * a.p[0].N;
+  const Problem& p = a.p[0];
+  const long long n = (long long)p.M * p.N;
   const dim3 grid((unsigned)((n / 4 + 255) / 256));
   if (dact)
-    return launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, (const void*)nullptr,
-                      (const float2*)a.saved, a.p[0].out, a.du, a.fp16);
-  return launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, (const float*)a.planes, a.S, n, a.residual,
-                    (const float2*)nullptr, a.p[0].out, (void*)nullptr, a.fp16);
+    return launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, (const float*)a.planes, p.S, n, (const void*)nullptr,
+                      (const float2*)a.saved, p.out, a.du, a.fp16);
+  return launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, (const float*)a.planes, p.S, n, a.residual,
+                    (const float2*)nullptr, p.out, (void*)nullptr, a.fp16);
 }
 
-Args args_of(const Plan& p, int M, int N, int KB, void* out, int dtype) {
+Problem problem_of(const Plan& p, int M, int N, int KB, void* out) {
+  return {M, N, p.mt, p.nt, out, KB, KB, p.S, 0, p.R, p.n_tile, 0, 0, 0};
+}
+
+Args args_of(const Problem& p, int dtype) {
   Args a = {};
-  a.p[0] = {M, N, p.mt, p.nt, out};
+  a.p[0] = p;
   a.np = 1;
-  a.KB = a.segKB = KB;
-  a.S = p.S;
-  a.R = p.R;
-  a.n_tile = p.n_tile;
   a.fp16 = dtype == MOE_FP16;
   return a;
+}
+
+// gradient of a weight matrix [N][M], summed over KB blocks of tokens
+Problem weight_gradient(int M, int N, int KB, void* out, int map, bool slim) {
+  const int n_tile = slim ? Form<true>::kAccCols : Form<false>::kAccCols;
+  return {M, N, (M + 4 * kAccRows - 1) / (4 * kAccRows), (N + n_tile - 1) / n_tile, out, KB, KB, 1, 0, kAccRows, n_tile, map, map, 1};
 }
 
 // Tensor map of one operand: contiguous in k ([rows][K]), boxes of 64 k x box rows, or in m / n ([K][rows]), boxes of
@@ -736,7 +810,7 @@ int kblocks(int K) { return (K + BK - 1) / BK; }
 Plan gu_plan(int T, int h, int f, int pairs) { return choose_plan(kGateUp, f, T, kblocks(h), false, pairs); }
 Plan down_plan(int T, int h, int f, int pairs) { return choose_plan(kPlain, h, T, kblocks(f), true, pairs); }
 Plan dact_plan(int T, int h, int f, int pairs) { return choose_plan(kDact, f, T, kblocks(h), true, pairs); }
-Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kDx, h, T, 2 * kblocks(f), true, pairs); }
+Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kGrads, h, T, 2 * kblocks(f), true, pairs); }
 
 // the saved buffer: (p, q), then a
 size_t pq_bytes(int T, int f) { return round256((size_t)T * f * sizeof(float2)); }
@@ -829,7 +903,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
     return MOE_OK;
   }
   Plan p = gu_plan(T, h, f, pairs);
-  Args a = args_of(p, f, T, kblocks(h), act, dtype);
+  Args a = args_of(problem_of(p, f, T, kblocks(h), act), dtype);
   a.saved = static_cast<float2*>(saved);
   Maps maps = {};
   FFN_MAP(map_k(&maps.a[0], W1, h, f, p.R));
@@ -837,7 +911,7 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   FFN_MAP(map_k(&maps.b[0], x, h, T, p.n_tile / 2));
   FFN_TRY("gate/up launch", saved ? launch_gemm<kGateUpSave>(maps, a, p.slim, pairs, st) : launch_gemm<kGateUp>(maps, a, p.slim, pairs, st));
   p = down_plan(T, h, f, pairs);
-  a = args_of(p, h, T, kblocks(f), y, dtype);
+  a = args_of(problem_of(p, h, T, kblocks(f), y), dtype);
   a.residual = residual;
   a.early = 1;
   a.planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
@@ -892,7 +966,7 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   Maps maps = {};
   // da = dy W2, and dg, du
   Plan p = dact_plan(T, h, f, pairs);
-  Args a = args_of(p, f, T, kblocks(h), dg, dtype);
+  Args a = args_of(problem_of(p, f, T, kblocks(h), dg), dtype);
   a.saved = static_cast<float2*>(const_cast<void*>(saved));
   a.du = du;
   a.planes = planes;
@@ -900,32 +974,28 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   FFN_MAP(map_k(&maps.b[0], dy, h, T, p.n_tile / 2));
   FFN_TRY("da launch", launch_gemm<kDact>(maps, a, p.slim, pairs, st));
   if (p.S > 1) FFN_TRY("join launch", launch_join(true, a, st));
-  // dx = dg W1 + du W3
+  // dx = dg W1 + du W3; dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
   p = dx_plan(T, h, f, pairs);
-  a = args_of(p, h, T, 2 * kblocks(f), dx, dtype);
-  a.segKB = kblocks(f);
+  a = args_of(problem_of(p, h, T, 2 * kblocks(f), dx), dtype);
+  a.p[0].segKB = kblocks(f);
+  a.p[1] = weight_gradient(h, f, kblocks(T), dW1, 2, p.slim);
+  a.p[2] = weight_gradient(h, f, kblocks(T), dW3, 3, p.slim);
+  a.p[3] = weight_gradient(f, h, kblocks(T), dW2, 4, p.slim);
+  a.np = 4;
   a.early = 1;
   a.planes = planes;
   FFN_MAP(map_mn(&maps.a[0], W1, h, f));
   FFN_MAP(map_mn(&maps.a[1], W3, h, f));
+  FFN_MAP(map_mn(&maps.a[2], x, h, T));
+  maps.a[3] = maps.a[2];
+  FFN_MAP(map_mn(&maps.a[4], act, f, T));
   FFN_MAP(map_k(&maps.b[0], dg, f, T, p.n_tile / 2));
   FFN_MAP(map_k(&maps.b[1], du, f, T, p.n_tile / 2));
-  FFN_TRY("dx launch", launch_gemm<kDx>(maps, a, p.slim, pairs, st));
+  FFN_MAP(map_mn(&maps.b[2], dg, f, T));
+  FFN_MAP(map_mn(&maps.b[3], du, f, T));
+  FFN_MAP(map_mn(&maps.b[4], dy, h, T));
+  FFN_TRY("gradients launch", launch_gemm<kGrads>(maps, a, p.slim, pairs, st));
   if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
-  // dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
-  a = args_of({kAccRows, 256, 1, 0, 0, false}, 0, 0, kblocks(T), nullptr, dtype);
-  a.np = 3;
-  const int rows = 4 * a.R;
-  a.p[0] = {h, f, (h + rows - 1) / rows, (f + a.n_tile - 1) / a.n_tile, dW1};
-  a.p[1] = {h, f, a.p[0].mt, a.p[0].nt, dW3};
-  a.p[2] = {f, h, (f + rows - 1) / rows, (h + a.n_tile - 1) / a.n_tile, dW2};
-  FFN_MAP(map_mn(&maps.a[0], x, h, T));
-  FFN_MAP(map_mn(&maps.a[2], act, f, T));
-  FFN_MAP(map_mn(&maps.b[0], dg, f, T));
-  FFN_MAP(map_mn(&maps.b[1], du, f, T));
-  FFN_MAP(map_mn(&maps.b[2], dy, h, T));
-  maps.a[1] = maps.a[0];
-  FFN_TRY("weight gradients launch", launch_gemm<kDw>(maps, a, false, pairs, st));
   return MOE_OK;
 }
 
@@ -944,6 +1014,7 @@ int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]) {
 
 int moe_operators_status(void) {
   int v = 0, zero = 0;
+  FFN_TRY("waiting for the device", cudaDeviceSynchronize());
   FFN_TRY("reading the status", cudaMemcpyFromSymbol(&v, g_status, sizeof(v)));
   if (!v) return MOE_OK;
   FFN_TRY("clearing the status", cudaMemcpyToSymbol(g_status, &zero, sizeof(zero)));
