@@ -379,8 +379,8 @@ def _operand(name, t, dtype, shape, index):
 def _on_device_of(x, dims, stream, body, *args):
     """body(device index, stream handle, *args) with the device of ``x`` current; memory that it takes from torch's
     allocator belongs to the stream that it launches on."""
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == dims and x.dtype in DTYPES):
-        raise MoeError(-1, "expected a %d-dimensional CUDA tensor of bf16, fp16 or fp32" % dims)
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == dims and x.dtype in DTYPES and x.is_contiguous()):
+        raise MoeError(-1, "expected a contiguous %d-dimensional CUDA tensor of bf16, fp16 or fp32" % dims)
     index = x.get_device()
     if stream is not None:
         if stream.device_index != index:
@@ -393,16 +393,21 @@ def _on_device_of(x, dims, stream, body, *args):
         return body(index, _raw_stream(index), *args)
 
 
+def _output(name, t, like, index, dtype=None):
+    """(address, tensor) of an output of ``like``'s shape, a new tensor where the caller gave none."""
+    if t is None:
+        t = torch.empty_like(like) if dtype is None else torch.empty_like(like, dtype=dtype)
+        return t.data_ptr(), t
+    return _operand(name, t, dtype or like.dtype, like.shape, index), t
+
+
 def _sum_buffer(x, residual, s, index):
     """Address of s (a new tensor where the caller gave none), and s itself."""
     if residual is None:
         if s is not None:
             raise MoeError(-1, "without a residual s is x itself")
         return None, x
-    if s is None:
-        s = torch.empty_like(x)
-        return s.data_ptr(), s
-    return _operand("s", s, x.dtype, x.shape, index), s
+    return _output("s", s, x, index)
 
 
 def add_rmsnorm(x, residual=None, gain=None, eps: float = 1e-5, out=None, s=None, rstd=None, stream=None):
@@ -417,13 +422,11 @@ def add_rmsnorm(x, residual=None, gain=None, eps: float = 1e-5, out=None, s=None
 def _add_rmsnorm(index, st, x, residual, gain, eps, out, s, rstd):
     T, h = shape = x.shape
     dt = x.dtype
-    xp, rp = _operand("x", x, dt, shape, index), _operand("residual", residual, dt, shape, index)
-    gp, tp = _operand("gain", gain, dt, (h,), index), _operand("rstd", rstd, torch.float32, (T,), index)
+    rp, gp = _operand("residual", residual, dt, shape, index), _operand("gain", gain, dt, (h,), index)
+    tp = _operand("rstd", rstd, torch.float32, (T,), index)
     sp, s = _sum_buffer(x, residual, s, index)
-    if out is None:
-        out = torch.empty_like(x)
-    op = _operand("out", out, dt, shape, index)
-    _check(load_library().moe_add_rmsnorm(xp, rp, gp, T, h, eps, DTYPES[dt], op, sp, tp, st))
+    op, out = _output("out", out, x, index)
+    _check(load_library().moe_add_rmsnorm(x.data_ptr(), rp, gp, T, h, eps, DTYPES[dt], op, sp, tp, st))
     return out, s
 
 
@@ -438,17 +441,14 @@ def add_rmsnorm_e4m3(x, residual=None, gain=None, eps: float = 1e-5, group: int 
 def _add_rmsnorm_e4m3(index, st, x, residual, gain, eps, group, q, scales, s):
     T, h = shape = x.shape
     dt = x.dtype
-    xp, rp = _operand("x", x, dt, shape, index), _operand("residual", residual, dt, shape, index)
-    gp = _operand("gain", gain, dt, (h,), index)
+    rp, gp = _operand("residual", residual, dt, shape, index), _operand("gain", gain, dt, (h,), index)
     sp, s = _sum_buffer(x, residual, s, index)
-    if q is None:
-        q = torch.empty_like(x, dtype=torch.float8_e4m3fn)
-    qp = _operand("q", q, torch.float8_e4m3fn, shape, index)
+    qp, q = _output("q", q, x, index, torch.float8_e4m3fn)
     n = h // group if group > 0 else 1
     if scales is None:
         scales = x.new_empty((T, n), dtype=torch.float32)
     cp = _operand("scales", scales, torch.float32, (T, n), index)
-    _check(load_library().moe_add_rmsnorm_e4m3(xp, rp, gp, T, h, eps, DTYPES[dt], group, qp, cp, sp, st))
+    _check(load_library().moe_add_rmsnorm_e4m3(x.data_ptr(), rp, gp, T, h, eps, DTYPES[dt], group, qp, cp, sp, st))
     return q, scales, s
 
 
@@ -459,25 +459,27 @@ def add_rmsnorm_backward(d_out, s, rstd, gain=None, d_s=None, dx=None, dgain=Non
     return _on_device_of(d_out, 2, stream, _add_rmsnorm_backward, d_out, s, rstd, gain, d_s, dx, dgain)
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(T: int, h: int, index: int) -> int:
+    """Bytes of the backward pass's workspace on this device, which is current."""
+    return int(load_library().moe_add_rmsnorm_backward_workspace(T, h))
+
+
 def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
     T, h = shape = d_out.shape
     dt = d_out.dtype
-    dp, sp = _operand("d_out", d_out, dt, shape, index), _operand("s", s, dt, shape, index)
-    ep, gp = _operand("d_s", d_s, dt, shape, index), _operand("gain", gain, dt, (h,), index)
-    tp = _operand("rstd", rstd, torch.float32, (T,), index)
-    if dx is None:
-        dx = torch.empty_like(d_out)
-    xp = _operand("dx", dx, dt, shape, index)
+    sp, ep = _operand("s", s, dt, shape, index), _operand("d_s", d_s, dt, shape, index)
+    gp, tp = _operand("gain", gain, dt, (h,), index), _operand("rstd", rstd, torch.float32, (T,), index)
+    xp, dx = _output("dx", dx, d_out, index)
     if gain is not None and dgain is None:
         dgain = torch.empty_like(gain)
-    lib = load_library()
     wp, n = None, 0
     if dgain is not None:
-        n = lib.moe_add_rmsnorm_backward_workspace(T, h)
+        n = _norm_workspace(T, h, index)
         ws = d_out.new_empty((n,), dtype=torch.uint8)
         wp = ws.data_ptr()
-    _check(lib.moe_add_rmsnorm_backward(dp, ep, sp, tp, gp, T, h, DTYPES[dt], xp,
-                                        _operand("dgain", dgain, dt, (h,), index), wp, n, st))
+    _check(load_library().moe_add_rmsnorm_backward(d_out.data_ptr(), ep, sp, tp, gp, T, h, DTYPES[dt], xp,
+                                                   _operand("dgain", dgain, dt, (h,), index), wp, n, st))
     return dx, dgain
 
 
@@ -511,16 +513,13 @@ def _ffn_sizes(x, W1):
 def _ffn_forward(index, st, x, W1, W3, W2, residual, y, saved):
     T, h, f = _ffn_sizes(x, W1)
     dt, shape = x.dtype, x.shape
-    xp = _operand("x", x, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
     w2, rp = _operand("W2", W2, dt, (h, f), index), _operand("residual", residual, dt, shape, index)
     n_saved, n, _ = _ffn_bytes(T, h, f, index)
     sp = _operand("saved", saved, torch.uint8, (n_saved,), index)
-    if y is None:
-        y = torch.empty_like(x)
-    yp = _operand("y", y, dt, shape, index)
+    yp, y = _output("y", y, x, index)
     ws = x.new_empty((n,), dtype=torch.uint8)
-    _check(load_library().moe_ffn_forward(xp, w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
+    _check(load_library().moe_ffn_forward(x.data_ptr(), w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
     return y
 
 
@@ -533,18 +532,15 @@ def ffn_backward(d_y, x, W1, W3, W2, saved, dx=None, dW1=None, dW3=None, dW2=Non
 def _ffn_backward(index, st, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2):
     T, h, f = _ffn_sizes(x, W1)
     dt, shape = x.dtype, x.shape
-    dp, xp = _operand("d_y", d_y, dt, shape, index), _operand("x", x, dt, shape, index)
+    dp = _operand("d_y", d_y, dt, shape, index)
     w1, w3 = _operand("W1", W1, dt, (f, h), index), _operand("W3", W3, dt, (f, h), index)
     n_saved, _, n = _ffn_bytes(T, h, f, index)
     w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.uint8, (n_saved,), index)
-    dx = torch.empty_like(x) if dx is None else dx
-    dW1 = torch.empty_like(W1) if dW1 is None else dW1
-    dW3 = torch.empty_like(W3) if dW3 is None else dW3
-    dW2 = torch.empty_like(W2) if dW2 is None else dW2
+    (xp, dx), (p1, dW1) = _output("dx", dx, x, index), _output("dW1", dW1, W1, index)
+    (p3, dW3), (p2, dW2) = _output("dW3", dW3, W3, index), _output("dW2", dW2, W2, index)
     ws = x.new_empty((n,), dtype=torch.uint8)
-    _check(load_library().moe_ffn_backward(dp, xp, w1, w3, w2, sp, T, h, f, DTYPES[dt], _operand("dx", dx, dt, shape, index),
-                                _operand("dW1", dW1, dt, (f, h), index), _operand("dW3", dW3, dt, (f, h), index),
-                                _operand("dW2", dW2, dt, (h, f), index), ws.data_ptr(), n, st))
+    _check(load_library().moe_ffn_backward(dp, x.data_ptr(), w1, w3, w2, sp, T, h, f, DTYPES[dt], xp, p1, p3, p2,
+                                           ws.data_ptr(), n, st))
     return dx, dW1, dW3, dW2
 
 
