@@ -71,6 +71,13 @@ void moe_test_set_free_bytes_limit(long long bytes);
  */
 int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]);
 
+/*
+ * The wait of moe_test_wait_expiry_pair (its leader) on the given stream, reported where the
+ * feed-forward block's kernels report theirs: the next moe_operators_status returns
+ * MOE_ERR_DEVICE_TIMEOUT once.  Errors: MOE_ERR_INVALID_ARG, MOE_ERR_ARCH, MOE_ERR_CUDA.
+ */
+int moe_test_operators_expiry(unsigned limit_us, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -129,6 +129,7 @@ __device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, int 
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copy_wait_but_one() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ float2 load8_shared(uint32_t addr) {
   float2 v;
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
@@ -514,6 +515,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
               store_cols<4>(wg, reinterpret_cast<uint16_t*>(p.out) + at, ld, c0, t.valid, in_m, lane);
               store_cols<4>(wu, reinterpret_cast<uint16_t*>(args.du) + at, ld, c0, t.valid, in_m, lane);
             }
+            copy_wait_all();  // nothing in flight when the CTA gives up
             if (!ok) break;
             continue;
           }
@@ -1009,6 +1011,17 @@ int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]) {
   const int kb = launch == 0 || launch == 2 ? kblocks(h) : kblocks(f) * (launch == 3 ? 2 : 1);
   const int v[6] = {p.R, p.n_tile, p.S, p.mt, p.nt, kb};
   for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  return MOE_OK;
+}
+
+int moe_test_operators_expiry(unsigned limit_us, void* cuda_stream) {
+  if (limit_us < 1 || limit_us > 100000) return set_error(MOE_ERR_INVALID_ARG, "limit_us = %u outside 1..100000", limit_us);
+  int rc = check_device();
+  if (rc) return rc;
+  void* status = nullptr;
+  FFN_TRY("the status word's address", cudaGetSymbolAddress(&status, g_status));
+  FFN_TRY("launch", launch_wait_expiry_pair(static_cast<int*>(status), (unsigned long long)limit_us * 1000ull, 0,
+                                            static_cast<cudaStream_t>(cuda_stream)));
   return MOE_OK;
 }
 

@@ -438,6 +438,20 @@ def test_rows_beyond_32_bit_offsets():
 
 
 @gpu
+def test_an_expired_wait_is_reported_once_and_leaves_the_operators_usable():
+    T, h, f = 300, 520, 1032
+    x, W1, W3, W2, _ = make(T, h, f, torch.bfloat16, seed=3)
+    y = binding.ffn_forward(x, W1, W3, W2)
+    lib = binding.load_library()
+    assert lib.moe_test_operators_expiry(0, None) == -1 and lib.moe_test_operators_expiry(100001, None) == -1
+    assert binding.operators_status(DEV) == 0
+    assert lib.moe_test_operators_expiry(1000, torch.cuda.current_stream().cuda_stream) == 0
+    assert binding.operators_status(DEV) == -5 and "expired" in binding.last_error()
+    assert binding.operators_status() == 0
+    assert torch.equal(binding.ffn_forward(x, W1, W3, W2), y) and binding.operators_status() == 0
+
+
+@gpu
 @pytest.mark.parametrize("T", [1, 50, 400])
 def test_prenorm_block_beside_routed_experts(T):
     """The operators as they are used together: residual addition and norm, the dense block as a shared expert whose
