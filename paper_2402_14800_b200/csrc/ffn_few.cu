@@ -86,8 +86,8 @@ ffn_gemv_gate_up_kernel(const void* x, const uint4* W1, const uint4* W3, int tok
       uint4 wg[4], wu[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        wg[k] = __ldcs(g + v + 32 * k);
-        wu[k] = __ldcs(u + v + 32 * k);
+        wg[k] = __ldcg(g + v + 32 * k);
+        wu[k] = __ldcg(u + v + 32 * k);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -100,7 +100,7 @@ ffn_gemv_gate_up_kernel(const void* x, const uint4* W1, const uint4* W3, int tok
       }
     }
     for (; v < nvec; v += 32) {
-      const uint4 wg = __ldcs(g + v), wu = __ldcs(u + v);
+      const uint4 wg = __ldcg(g + v), wu = __ldcg(u + v);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         ag[t] = dot8<T>(s_x[t * nvec + v], wg, ag[t]);
@@ -126,7 +126,7 @@ ffn_gemv_down_kernel(const T* act, const uint4* W2, const T* residual, int token
   if (n < h) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (lane + 32 * k < nvec) w[k] = __ldcs(W2 + (size_t)n * nvec + lane + 32 * k);
+      if (lane + 32 * k < nvec) w[k] = __ldcg(W2 + (size_t)n * nvec + lane + 32 * k);
   }
   pdl_wait();
   pdl_launch_dependents();
@@ -138,7 +138,7 @@ ffn_gemv_down_kernel(const T* act, const uint4* W2, const T* residual, int token
       if (!first || v != lane) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if (v + 32 * k < nvec) w[k] = __ldcs(row + v + 32 * k);
+          if (v + 32 * k < nvec) w[k] = __ldcg(row + v + 32 * k);
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
@@ -248,8 +248,8 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) ffn_mma_kernel(const MmaAr
     for (int i = 0; i < 4; ++i) {
       const int v = (u + i) * 4 + kq;
       const bool in = u + i < u1 && v < nvec;
-      w[2 * i] = in && m0 < hi ? __ldcs(a.A0 + (size_t)m0 * nvec + v) : make_uint4(0, 0, 0, 0);
-      w[2 * i + 1] = in && m1 < hi ? __ldcs(a.A1 + (size_t)m1 * nvec + v) : make_uint4(0, 0, 0, 0);
+      w[2 * i] = in && m0 < hi ? __ldcg(a.A0 + (size_t)m0 * nvec + v) : make_uint4(0, 0, 0, 0);
+      w[2 * i + 1] = in && m1 < hi ? __ldcg(a.A1 + (size_t)m1 * nvec + v) : make_uint4(0, 0, 0, 0);
     }
   };
   uint4 w[8];
@@ -262,7 +262,9 @@ __global__ void __launch_bounds__(32 * kMostWarps, 1) ffn_mma_kernel(const MmaAr
     s_x[i] = v < nvec ? ld_l2(reinterpret_cast<const uint4*>(a.x) + (size_t)t * nvec + v) : make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
-  for (int tile = tile0; tile < tiles; tile += tile_step) {  // more than one round only without splits
+  // More than one round only without splits.  With them every warp goes through the one round and its barriers: a block
+  // of fewer tiles than the largest has warps whose rows all lie behind its last, which load and store nothing.
+  for (int tile = tile0; a.splits > 1 ? tile == tile0 : tile < tiles; tile += tile_step) {
     float d[NB][4] = {};
     for (int u = u0; u < u1; u += 4) {
       if (u != u0 || tile != tile0) fetch(w, tile, u);

@@ -892,9 +892,17 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   if (overlap(y, n, x, n) || overlap(y, n, W1, w) || overlap(y, n, W3, w) || overlap(y, n, W2, w) ||
       overlap(y, n, saved, n_saved) || (residual != y && overlap(y, n, residual, n)))
     return set_error(MOE_ERR_INVALID_ARG, "y overlaps another tensor (only the residual itself is allowed)");
+  const void* ins[5] = {x, W1, W3, W2, residual};
+  const size_t in_bytes[5] = {n, w, w, w, n};
+  for (int i = 0; i < 5; ++i)
+    if (overlap(ins[i], in_bytes[i], saved, n_saved)) return set_error(MOE_ERR_INVALID_ARG, "saved overlaps an input");
   const size_t need = moe_ffn_forward_workspace(T, h, f);
   if (!workspace || workspace_bytes < need)
     return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need);
+  for (int i = 0; i < 5; ++i)
+    if (overlap(ins[i], in_bytes[i], workspace, need)) return set_error(MOE_ERR_INVALID_ARG, "the workspace overlaps a tensor");
+  if (overlap(y, n, workspace, need) || overlap(saved, n_saved, workspace, need))
+    return set_error(MOE_ERR_INVALID_ARG, "the workspace overlaps a tensor");
   if ((rc = check_device())) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const int pairs = sm_count() / 2;
@@ -958,6 +966,9 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   const size_t need = moe_ffn_backward_workspace(T, h, f);
   if (!workspace || workspace_bytes < need)
     return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0, need);
+  for (int i = 0; i < 6; ++i)
+    if (overlap(ins[i], in_bytes[i], workspace, need) || (i < 4 && overlap(outs[i], out_bytes[i], workspace, need)))
+      return set_error(MOE_ERR_INVALID_ARG, "the workspace overlaps a tensor");
   if ((rc = check_device())) return rc;
   const int pairs = sm_count() / 2;
   char* ws = static_cast<char*>(workspace);

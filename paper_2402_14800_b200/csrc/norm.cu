@@ -51,14 +51,6 @@ template <typename T, int E> struct Vec {
     raw = __ldcg(reinterpret_cast<const decltype(raw)*>(p));
   }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<decltype(raw)*>(p) = raw; }
-  // the same for data that L2 cannot hold until somebody reads it again
-  __device__ __forceinline__ void load(const T* p, bool stream) {
-    raw = stream ? __ldcs(reinterpret_cast<const decltype(raw)*>(p)) : __ldcg(reinterpret_cast<const decltype(raw)*>(p));
-  }
-  __device__ __forceinline__ void store(T* p, bool stream) const {
-    if (stream) __stcs(reinterpret_cast<decltype(raw)*>(p), raw);
-    else *reinterpret_cast<decltype(raw)*>(p) = raw;
-  }
 };
 
 // Sum (or maximum of non-negative values) over the TPR threads of a row; every thread gets the same bits.
@@ -90,7 +82,6 @@ struct NormArgs {
   float* scales;     // e4m3
   int T, h, group;   // group: 0 = one scale a row, else 128
   float eps;
-  bool stream;       // the tensors together are larger than L2 can make use of
 };
 
 // Rows per block: 256 / 32 with a warp a row, else one.
@@ -162,8 +153,8 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
         const int v = i * TPR + lane;
         if (t < a.T && v < nvec) {
           const size_t o = (size_t)t * h + (size_t)v * E;
-          x[i].load(reinterpret_cast<const T*>(a.x) + o, a.stream);
-          if (add) r[i].load(reinterpret_cast<const T*>(a.r) + o, a.stream);
+          x[i].load(reinterpret_cast<const T*>(a.x) + o);
+          if (add) r[i].load(reinterpret_cast<const T*>(a.r) + o);
         }
       }
     };
@@ -195,11 +186,11 @@ __global__ void __launch_bounds__(Shape<TPR>::kThreads) add_rmsnorm_kernel(const
           const int v = i * TPR + lane;
           if (!live || v >= nvec) continue;
           const size_t o = (size_t)row * h + (size_t)v * E;
-          if (add) s[i].store(reinterpret_cast<T*>(a.s) + o, a.stream);
+          if (add) s[i].store(reinterpret_cast<T*>(a.s) + o);
           V y;
 #pragma unroll
           for (int k = 0; k < E; ++k) y.set(k, s[i].get(k) * rstd * gain[i].get(k));
-          y.store(reinterpret_cast<T*>(a.out) + o, a.stream);
+          y.store(reinterpret_cast<T*>(a.out) + o);
         }
       } else {
         float mx[NV], all = 0.f;
@@ -616,14 +607,16 @@ int forward(const void* x, const void* residual, const void* gain, int T, int h,
     if (p && (q || p != out) && overlap(p, n, out, n_out))
       return set_error(MOE_ERR_INVALID_ARG, "the output overlaps an input");
   }
+  const size_t n_scales = q ? (size_t)T * (group ? h / group : 1) * sizeof(float) : 0, n_rstd = (size_t)T * sizeof(float);
+  const void* whole[5] = {x, residual, out, s, gain};
+  const size_t bytes[5] = {n, n, n_out, n, h * e};
+  for (int i = 0; i < 5; ++i)
+    if (overlap(whole[i], bytes[i], rstd, n_rstd) || overlap(whole[i], bytes[i], scales, n_scales))
+      return set_error(MOE_ERR_INVALID_ARG, "rstd or scales overlaps another tensor");
   if (overlap(s, n, out, n_out)) return set_error(MOE_ERR_INVALID_ARG, "s and the output overlap");
   if (overlap(gain, h * e, out, n_out) || overlap(gain, h * e, s, n))
     return set_error(MOE_ERR_INVALID_ARG, "the gain overlaps an output");
-  // Evict-first loads and stores from four times L2's 126 MB on: 32768 x 4096 bf16, 1.07 GB, 180.8 -> 177.2 us.  With
-  // less the next operator still finds some of what was written: forward and backward of 8192 x 4096, 268 MB, 92.0 ->
-  // 94.9 us.
-  const bool stream = 4 * n > ((size_t)504 << 20);
-  NormArgs a = {x, residual, gain, out, s, rstd, scales, T, h, group, eps, stream};
+  NormArgs a = {x, residual, gain, out, s, rstd, scales, T, h, group, eps};
   const cudaError_t err = dtype == MOE_BF16 ? launch_norm_type<__nv_bfloat16>(a, q, st)
                           : dtype == MOE_FP16 ? launch_norm_type<__half>(a, q, st) : launch_norm_type<float>(a, q, st);
   if (err != cudaSuccess) return set_error(MOE_ERR_CUDA, "add_rmsnorm launch: %s", cudaGetErrorString(err));
@@ -682,6 +675,12 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
   if (overlap(dgain, h * e, d_out, n) || overlap(dgain, h * e, s, n) || overlap(dgain, h * e, dx, n) ||
       overlap(dgain, h * e, gain, h * e) || overlap(dgain, h * e, d_s, n))
     return set_error(MOE_ERR_INVALID_ARG, "dgain overlaps another tensor");
+  const size_t n_ws = dgain ? moe_add_rmsnorm_backward_workspace(T, h) : 0, n_rstd = (size_t)T * sizeof(float);
+  const void* whole[7] = {d_out, d_s, s, gain, rstd, dx, dgain};
+  const size_t bytes[7] = {n, n, n, h * e, n_rstd, n, h * e};
+  for (int i = 0; i < 7; ++i)
+    if ((n_ws && overlap(whole[i], bytes[i], workspace, n_ws)) || (i > 4 && overlap(whole[i], bytes[i], rstd, n_rstd)))
+      return set_error(MOE_ERR_INVALID_ARG, "the workspace overlaps a tensor, or a gradient rstd");
   NormBwdArgs a = {d_out, d_s, s, gain, rstd, dx, nullptr, T, h};
   float* partial = static_cast<float*>(workspace);
   const cudaError_t err = dtype == MOE_BF16   ? launch_bwd_type<__nv_bfloat16>(a, dgain, partial, st)

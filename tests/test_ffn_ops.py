@@ -50,6 +50,10 @@ def test_refuses_bad_arguments_without_a_device(lib):
         assert fwd(y={"x": p[0], "W1": p[1], "W3": p[2], "W2": p[3], "saved": p[6]}[k]) == -1, k
         assert "overlap" in binding.last_error()
     assert fwd(y=ctypes.c_void_p((5 << 24) + 64)) == -1 and "overlap" in binding.last_error()
+    for i, k in enumerate(names[:-1]):
+        assert fwd(ws=p[i]) == -1 and "workspace overlaps" in binding.last_error(), k
+        if k not in ("y", "saved"):
+            assert fwd(saved=p[i]) == -1 and "saved overlaps" in binding.last_error(), k
     assert fwd(dt=2) == -1 and "dtype" in binding.last_error()  # the tensor cores' 16-bit types
     assert fwd(h=68) == -2 and fwd(f=4) == -2 and fwd(h=0) == -2 and fwd(f=(1 << 20) + 8) == -2
     assert fwd(T=-1) == -1 and fwd(T=(1 << 24) + 1) == -1
@@ -71,6 +75,8 @@ def test_refuses_bad_arguments_without_a_device(lib):
         for i in range(6):
             assert bwd(**{k: p[i]}) == -1 and "overlaps an input" in binding.last_error()
     assert bwd(dW1=p[8]) == -1 and "two gradients" in binding.last_error()
+    for i in range(10):
+        assert bwd(ws=p[i]) == -1 and "workspace overlaps" in binding.last_error(), names_b[i]
     assert bwd(ws=None) == -1 and bwd(n=100) == -1 and "workspace" in binding.last_error()
     assert bwd(dt=2) == -1 and bwd(h=12) == -2 and bwd(T=-1) == -1
     assert lib.moe_ffn_saved_bytes(0, 64) == 0 and lib.moe_ffn_saved_bytes(3, 60) == 0
@@ -197,7 +203,8 @@ SIZES = [(1, 8, 8), (3, 64, 8), (2, 8, 200), (1, 128, 448), (100, 128, 448), (31
          (256, 256, 512), (257, 264, 520), (300, 2048, 4096), (611, 2040, 5464), (1025, 512, 1032), (2500, 136, 72)]
 FEW = [(2, 4096, 14336), (3, 4096, 14336), (4, 40, 24), (5, 128, 448), (7, 4096, 14336), (8, 2040, 5464), (9, 1000, 2728),
        (16, 2048, 4096), (24, 264, 1032), (32, 1024, 2048), (33, 640, 1032), (50, 72, 1528), (64, 512, 1024), (64, 1528, 8),
-       (40, 8, 1528), (12, 4096, 72), (6, 72, 14336)]
+       (40, 8, 1528), (12, 4096, 72), (6, 72, 14336),
+       (5, 2400, 1200), (20, 2400, 1200)]  # blocks of unequal numbers of tiles
 
 
 @gpu
@@ -483,3 +490,46 @@ def test_prenorm_block_beside_routed_experts(T):
     want_x = dy.double() + root * (up - hat * (up * hat).mean(1, keepdim=True))
     assert bool(((dx.double() - want_x).abs() <= 2.0 ** -8 * want_x.abs() + 1e-4).all())
     layer.close()
+
+
+FRESH_PROCESS = """
+import torch
+from paper_2402_14800_b200 import binding
+T, h, f = %d, 256, 512
+torch.manual_seed(0)
+x, r, dy = (torch.randn((T, h), device="cuda").bfloat16() for _ in range(3))
+W1, W3, W2 = (torch.randn(s, device="cuda").mul_(0.06).bfloat16() for s in ((f, h), (f, h), (h, f)))
+gain = torch.ones(h, device="cuda").bfloat16()
+rstd = torch.empty(T, device="cuda")
+torch.cuda.synchronize()
+
+def step():
+    n, s = binding.add_rmsnorm(x, r, gain, rstd=rstd)
+    q, c, _ = binding.add_rmsnorm_e4m3(x, r, gain)
+    saved = binding.ffn_saved(T, f, x.device)
+    y = binding.ffn_forward(n, W1, W3, W2, residual=s, saved=saved)
+    y2 = binding.ffn_forward(n, W1, W3, W2)
+    dn, *dW = binding.ffn_backward(dy, n, W1, W3, W2, saved)
+    return n, s, q.float(), c, y, y2, dn, *dW, *binding.add_rmsnorm_backward(dn, s, rstd, gain, d_s=dy)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = step()
+for _ in range(2):
+    x.normal_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, step()))
+print("replayed")
+"""
+
+
+@gpu
+@pytest.mark.parametrize("T", [1, 5, 100, 300])
+def test_the_first_call_of_a_process_may_be_captured(T):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FRESH_PROCESS % T], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "replayed" in r.stdout, r.stdout + r.stderr

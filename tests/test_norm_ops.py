@@ -49,6 +49,8 @@ def test_refuses_bad_arguments_without_a_device(lib):
     assert fwd(s=ctypes.c_void_p(0x100000 + 128)) == -1 and "overlap" in binding.last_error()
     assert fwd(s=p[3]) == -1 and "overlap" in binding.last_error()
     assert fwd(g=p[3]) == -1 and "gain" in binding.last_error()
+    for k in range(5):
+        assert fwd(rstd=p[k]) == -1 and "rstd" in binding.last_error()
     assert fwd(T=0) == 0 and fwd(T=0, x=None, out=None) == 0
 
     def q8(group=0, h=256, q=p[3], scales=p[5], s=p[4]):
@@ -56,6 +58,7 @@ def test_refuses_bad_arguments_without_a_device(lib):
 
     assert q8(group=64) == -1 and q8(group=-1) == -1 and q8(group=128, h=200) == -2
     assert q8(scales=None) == -1 and "scales" in binding.last_error()
+    assert q8(scales=p[3]) == -1 and q8(scales=p[0]) == -1 and "scales overlaps" in binding.last_error()
     assert q8(q=p[0]) == -1 and "overlap" in binding.last_error()  # no 8-bit output in place
 
     def bwd(d=p[0], e=p[1], s=p[2], rstd=p[3], g=p[4], T=4, h=64, dt=0, dx=p[5], dg=p[6], ws=p[7], n=1 << 30):
@@ -69,6 +72,10 @@ def test_refuses_bad_arguments_without_a_device(lib):
     assert bwd(n=64 * 4 - 1) == -1 and "workspace" in binding.last_error()
     assert bwd(dx=p[0]) == -1 and bwd(dx=p[2]) == -1 and bwd(dx=ctypes.c_void_p(0x200000 + 128)) == -1
     assert bwd(dg=p[4]) == -1 and bwd(dg=p[5]) == -1
+    for k in range(7):
+        assert bwd(ws=p[k]) == -1 and "workspace overlaps" in binding.last_error()
+    for k in ("dx", "dg"):
+        assert bwd(**{k: p[3]}) == -1 and "rstd" in binding.last_error()
     assert bwd(dt=9) == -1 and bwd(h=0) == -2 and bwd(T=-2) == -1
     assert bwd(T=0, dg=None) == 0
     assert lib.moe_add_rmsnorm_backward_workspace(0, 64) == 0 and lib.moe_add_rmsnorm_backward_workspace(4, 0) == 0
