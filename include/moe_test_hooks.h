@@ -65,7 +65,8 @@ void moe_test_set_free_bytes_limit(long long bytes);
 /*
  * Host side only.  Tile and split that a launch of the feed-forward block takes on a
  * machine of `pairs` pairs of multiprocessors: launch = 0 gate/up, 1 down,
- * 2 the activation's gradient, 3 the input's gradient; plan[6] receives rows a CTA
+ * 2 the activation's gradient, 3 the input's gradient, 4 the weights' gradients (tiles
+ * 0: they follow from the matrix); plan[6] receives rows a CTA
  * and accumulator, columns of an item, k-splits, row tiles, column tiles, k-blocks
  * of 64 in the contraction.  Errors: MOE_ERR_INVALID_ARG.
  */

@@ -75,6 +75,7 @@ struct Problem {
   int R, n_tile;  // rows of A a CTA and accumulator loads, columns of an item
   int a0, b0;     // tensor maps of the first segment
   int bmn;        // B contiguous in n (weights' gradients)
+  float* planes;  // S > 1: [S][N][M] partial sums
 };
 
 struct Args {
@@ -86,7 +87,6 @@ struct Args {
   const void* residual;       // kPlain
   float2* saved;              // [N][M] (p, q): written by kGateUpSave, read by kDact
   void* du;                   // kDact, beside out = dg
-  float* planes;              // S > 1: [S][N][M] partial sums
   int early;                  // A is no earlier launch of this call's output: its first stages may be read ahead
 };
 
@@ -547,7 +547,7 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
               if (c0 >= t.valid) continue;
               const long long at = (long long)(t.n0 + c0) * ld + m0;
               if (p.S > 1) {
-                float* o = args.planes + (long long)t.ks * p.N * ld + at + lane;
+                float* o = p.planes + (long long)t.ks * p.N * ld + at + lane;
 #pragma unroll
                 for (int c = 0; c < 16; ++c) {
                   if (in_m && c0 + c < t.valid) *o = __uint_as_float(v[i][c]);
@@ -580,32 +580,46 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
 }
 
 // Sum of the S planes of a split launch in their order, and what the epilogue would have done with it: four
-// neighbouring m a thread.
-template <bool DACT>
-__global__ void __launch_bounds__(256) ffn_join_kernel(const float* planes, int S, long long n, const void* residual,
-                                                       const float2* saved, void* out, void* du, int fp16) {
-  pdl_wait();
-  pdl_launch_dependents();  // behind the wait: the launch that follows may read the weights ahead
-  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i >= n) return;
+// neighbouring m a thread, a problem of the launch for each blockIdx.y.
+struct Join {
+  const float* planes[4];
+  long long n[4];  // outputs of a problem
+  int S[4];        // 1: nothing to do
+  void* out[4];
+  const void* residual;
+  const float2* saved;  // da: the problem's outputs are dg and du
+  void* du;
+  int fp16;
+};
+
+__device__ __forceinline__ float4 sum_planes(const float* planes, int S, long long n, long long i) {
   float4 v = ld_l2(reinterpret_cast<const float4*>(planes + i));
   for (int s = 1; s < S; ++s) {
     const float4 w = ld_l2(reinterpret_cast<const float4*>(planes + (long long)s * n + i));
     v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
   }
+  return v;
+}
+
+template <bool DACT> __global__ void __launch_bounds__(256) ffn_join_kernel(const __grid_constant__ Join a) {
+  pdl_wait();
+  pdl_launch_dependents();  // behind the wait: the launch that follows may read the weights ahead
+  const int p = DACT ? 0 : blockIdx.y, fp16 = a.fp16;
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= a.n[p] || a.S[p] == 1) return;
+  float4 v = sum_planes(a.planes[p], a.S[p], a.n[p], i);
+  uint16_t* out = reinterpret_cast<uint16_t*>(a.out[p]) + i;
   if constexpr (!DACT) {
-    if (residual) {
-      const uint2 r = __ldcg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(residual) + i));
+    if (a.residual) {
+      const uint2 r = __ldcg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(a.residual) + i));
       const float2 r0 = unpack16(r.x, fp16), r1 = unpack16(r.y, fp16);
       v.x += r0.x; v.y += r0.y; v.z += r1.x; v.w += r1.y;
     }
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) =
-        make_uint2(pack16(v.x, v.y, fp16), pack16(v.z, v.w, fp16));
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack16(v.x, v.y, fp16), pack16(v.z, v.w, fp16));
   } else {
-    const float4 s0 = ld_l2(reinterpret_cast<const float4*>(saved + i)), s1 = ld_l2(reinterpret_cast<const float4*>(saved + i) + 1);
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(out) + i) =
-        make_uint2(pack16(v.x * s0.x, v.y * s0.z, fp16), pack16(v.z * s1.x, v.w * s1.z, fp16));
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(du) + i) =
+    const float4 s0 = ld_l2(reinterpret_cast<const float4*>(a.saved + i)), s1 = ld_l2(reinterpret_cast<const float4*>(a.saved + i) + 1);
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack16(v.x * s0.x, v.y * s0.z, fp16), pack16(v.z * s1.x, v.w * s1.z, fp16));
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.du) + i) =
         make_uint2(pack16(v.x * s0.y, v.y * s0.w, fp16), pack16(v.z * s1.y, v.w * s1.w, fp16));
   }
 }
@@ -694,7 +708,7 @@ Plan search_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
           return kbs * std::max(std::max(4.6 * n_tile, own), std::max(l2, hbm)) + 1500.0 + (gate_up(kind) ? 16.0 : 6.0) * n_tile;
         };
         double cost = full * (full ? round(pairs) : 0.0) + (rest ? round(rest) : 0.0);
-        if (S > 1) cost += 6000.0 + (double)S * N * M * 8 / 7000.0;
+        if (S > 1) cost += 4500.0 + (double)S * N * M * 8 / 7000.0;
         if (cost < best_cost) {
           best_cost = cost;
           best = {R, n_tile, S, mt, nt, slim};
@@ -705,18 +719,43 @@ Plan search_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   return best;
 }
 
+// The weights' gradients, three problems of one tile: 512 x 256 where they fill the machine, smaller tiles and splits
+// over the tokens where h and f are small and the tokens many.  8192 tokens of (h 128, f 448) in 512 x 256 tiles are five
+// items of 128 k-blocks.
+Plan search_weights_plan(int T, int h, int f, int pairs, bool slim) {
+  const int KB = (T + BK - 1) / BK;
+  Plan best = {};
+  double best_cost = 1e300;
+  for (int n = slim ? Form<true>::kAccCols : Form<false>::kAccCols; n >= 32; n >>= 1)
+    for (int R = kAccRows; R >= 64; R -= 64)
+      for (int S = 1; S <= 16 && (S == 1 || KB / S >= 2); ++S) {
+        const int kbs = (KB + S - 1) / S;
+        if ((KB + kbs - 1) / kbs != S) continue;
+        auto tiles = [&](int M, int N) { return (long long)((M + 4 * R - 1) / (4 * R)) * ((N + n - 1) / n); };
+        const long long items = S * (2 * tiles(h, f) + tiles(f, h));
+        if (S > 1 && items > 4 * pairs) break;
+        double cost = (double)((items + pairs - 1) / pairs) * (kbs * std::max(800.0, 4.6 * n) + 2000.0 + 8.0 * n);
+        if (S > 1) cost += 4500.0 + 3.0 * S * h * f * 8 / 7000.0;
+        if (cost < best_cost) {
+          best_cost = cost;
+          best = {R, n, S, 0, 0, slim};
+        }
+      }
+  return best;
+}
+
 // The same, remembered for the sizes that this thread asked about last: a search takes 1 to 8 us of the host, and a call
-// needs each plan two or three times.
+// needs each plan two or three times.  Kind -1, -2: the weights' gradients, -2 in the slim form (M: h, N: tokens, KB: f).
 Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
   struct Known {
     int kind, M, N, KB, pairs;
     Plan plan;
   };
-  static thread_local Known known[16] = {};
+  static thread_local Known known[32] = {};
   const unsigned hash = (unsigned)M * 0x9e3779b1u ^ (unsigned)N * 0x85ebca6bu ^ (unsigned)KB * 0xc2b2ae35u ^ (unsigned)kind * 0x27d4eb2fu;
-  Known& k = known[(hash >> 16) & 15u];
+  Known& k = known[(hash >> 16) & 31u];
   if (k.kind != kind || k.M != M || k.N != N || k.KB != KB || k.pairs != pairs)
-    k = {kind, M, N, KB, pairs, search_plan(kind, M, N, KB, may_split, pairs)};
+    k = {kind, M, N, KB, pairs, kind < 0 ? search_weights_plan(N, M, KB, pairs, may_split) : search_plan(kind, M, N, KB, may_split, pairs)};
   return k.plan;
 }
 
@@ -741,7 +780,7 @@ template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a
     const Problem &x = a.p[0], &w = a.p[1];
     const int n = x.mt * x.nt * x.S, grid = std::min(items, pairs);
     a.first = n < grid ? n : 0;
-    a.skip = a.first ? (int)(x.kbs * std::max(4.6 * x.n_tile, 600.0) / std::max(4.6 * w.n_tile * w.kbs + 4000.0, 9000.0)) : 0;
+    a.skip = a.first ? (int)(x.kbs * std::max(4.6 * x.n_tile, 600.0) / std::max(std::max(4.6 * w.n_tile, 800.0) * w.kbs + 4000.0, 9000.0)) : 0;
   }
   static std::atomic<unsigned long long> set{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
@@ -773,19 +812,29 @@ template <int KIND> cudaError_t launch_gemm(const Maps& maps, Args& a, bool slim
   return launch_form<KIND, false>(maps, a, pairs, st);
 }
 
+// nothing to do where no problem of the launch was split
 cudaError_t launch_join(bool dact, const Args& a, cudaStream_t st) {
-  const Problem& p = a.p[0];
-  const long long n = (long long)p.M * p.N;
-  const dim3 grid((unsigned)((n / 4 + 255) / 256));
-  if (dact)
-    return launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, (const float*)a.planes, p.S, n, (const void*)nullptr,
-                      (const float2*)a.saved, p.out, a.du, a.fp16);
-  return launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, (const float*)a.planes, p.S, n, a.residual,
-                    (const float2*)nullptr, p.out, (void*)nullptr, a.fp16);
+  Join j = {};
+  long long most = 0;
+  for (int i = 0; i < a.np; ++i) {
+    const Problem& p = a.p[i];
+    j.planes[i] = p.planes;
+    j.n[i] = (long long)p.M * p.N;
+    j.S[i] = p.S;
+    j.out[i] = p.out;
+    if (p.S > 1) most = std::max(most, j.n[i]);
+  }
+  if (!most) return cudaSuccess;
+  j.residual = a.residual;
+  j.saved = a.saved;
+  j.du = a.du;
+  j.fp16 = a.fp16;
+  const dim3 grid((unsigned)((most / 4 + 255) / 256), (unsigned)a.np);
+  return dact ? launch_pdl(ffn_join_kernel<true>, grid, dim3(256), 0, st, j) : launch_pdl(ffn_join_kernel<false>, grid, dim3(256), 0, st, j);
 }
 
 Problem problem_of(const Plan& p, int M, int N, int KB, void* out) {
-  return {M, N, p.mt, p.nt, out, KB, KB, p.S, 0, p.R, p.n_tile, 0, 0, 0};
+  return {M, N, p.mt, p.nt, out, KB, KB, p.S, 0, p.R, p.n_tile, 0, 0, 0, nullptr};
 }
 
 Args args_of(const Problem& p, int dtype) {
@@ -797,9 +846,8 @@ Args args_of(const Problem& p, int dtype) {
 }
 
 // gradient of a weight matrix [N][M], summed over KB blocks of tokens
-Problem weight_gradient(int M, int N, int KB, void* out, int map, bool slim) {
-  const int n_tile = slim ? Form<true>::kAccCols : Form<false>::kAccCols;
-  return {M, N, (M + 4 * kAccRows - 1) / (4 * kAccRows), (N + n_tile - 1) / n_tile, out, KB, KB, 1, 0, kAccRows, n_tile, map, map, 1};
+Problem weight_gradient(const Plan& p, int M, int N, int KB, void* out, int map) {
+  return {M, N, (M + 4 * p.R - 1) / (4 * p.R), (N + p.n_tile - 1) / p.n_tile, out, KB, KB, p.S, 0, p.R, p.n_tile, map, map, 1, nullptr};
 }
 
 // Tensor map of one operand: contiguous in k ([rows][K]), boxes of 64 k x box rows, or in m / n ([K][rows]), boxes of
@@ -813,11 +861,15 @@ Plan gu_plan(int T, int h, int f, int pairs) { return choose_plan(kGateUp, f, T,
 Plan down_plan(int T, int h, int f, int pairs) { return choose_plan(kPlain, h, T, kblocks(f), true, pairs); }
 Plan dact_plan(int T, int h, int f, int pairs) { return choose_plan(kDact, f, T, kblocks(h), true, pairs); }
 Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kGrads, h, T, 2 * kblocks(f), true, pairs); }
+Plan weights_plan(int T, int h, int f, int pairs) {
+  const bool slim = dx_plan(T, h, f, pairs).slim;  // one launch, one form
+  return choose_plan(slim ? -2 : -1, h, T, f, slim, pairs);
+}
 
 // the saved buffer: (p, q), then a
 size_t pq_bytes(int T, int f) { return round256((size_t)T * f * sizeof(float2)); }
 
-size_t plane_bytes(const Plan& p, int T, int M) { return p.S > 1 ? round256((size_t)p.S * T * M * sizeof(float)) : 0; }
+size_t plane_bytes(const Plan& p, int N, int M) { return p.S > 1 ? round256((size_t)p.S * N * M * sizeof(float)) : 0; }
 
 int check_block(int T, int h, int f, int dtype) {
   if (dtype != MOE_BF16 && dtype != MOE_FP16)
@@ -876,7 +928,8 @@ size_t moe_ffn_backward_workspace(int T, int h, int f) {
   if (T < 1 || check_block(T, h, f, MOE_BF16)) return 0;
   const int pairs = sm_count() / 2;
   return 2 * round256((size_t)T * f * 2) +
-         std::max(plane_bytes(dact_plan(T, h, f, pairs), T, f), plane_bytes(dx_plan(T, h, f, pairs), T, h));
+         std::max(plane_bytes(dact_plan(T, h, f, pairs), T, f),
+                  plane_bytes(dx_plan(T, h, f, pairs), T, h) + 3 * plane_bytes(weights_plan(T, h, f, pairs), f, h));
 }
 
 int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2, const void* residual, int T, int h, int f,
@@ -924,11 +977,11 @@ int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W
   a = args_of(problem_of(p, h, T, kblocks(f), y), dtype);
   a.residual = residual;
   a.early = 1;
-  a.planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
+  a.p[0].planes = reinterpret_cast<float*>(ws + round256((size_t)T * f * 2));
   FFN_MAP(map_k(&maps.a[0], W2, f, h, p.R));
   FFN_MAP(map_k(&maps.b[0], act, f, T, p.n_tile / 2));
   FFN_TRY("down launch", launch_gemm<kPlain>(maps, a, p.slim, pairs, st));
-  if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
+  FFN_TRY("join launch", launch_join(false, a, st));
   return MOE_OK;
 }
 
@@ -975,28 +1028,32 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   const size_t part = round256((size_t)T * f * 2);
   const void* act = static_cast<const char*>(saved) + pq_bytes(T, f);
   void *dg = ws, *du = ws + part;
-  float* planes = reinterpret_cast<float*>(ws + 2 * part);
+  char* planes = ws + 2 * part;
   Maps maps = {};
   // da = dy W2, and dg, du
   Plan p = dact_plan(T, h, f, pairs);
   Args a = args_of(problem_of(p, f, T, kblocks(h), dg), dtype);
   a.saved = static_cast<float2*>(const_cast<void*>(saved));
   a.du = du;
-  a.planes = planes;
+  a.p[0].planes = reinterpret_cast<float*>(planes);
   FFN_MAP(map_mn(&maps.a[0], W2, f, h));
   FFN_MAP(map_k(&maps.b[0], dy, h, T, p.n_tile / 2));
   FFN_TRY("da launch", launch_gemm<kDact>(maps, a, p.slim, pairs, st));
-  if (p.S > 1) FFN_TRY("join launch", launch_join(true, a, st));
+  FFN_TRY("join launch", launch_join(true, a, st));
   // dx = dg W1 + du W3; dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
   p = dx_plan(T, h, f, pairs);
   a = args_of(problem_of(p, h, T, 2 * kblocks(f), dx), dtype);
   a.p[0].segKB = kblocks(f);
-  a.p[1] = weight_gradient(h, f, kblocks(T), dW1, 2, p.slim);
-  a.p[2] = weight_gradient(h, f, kblocks(T), dW3, 3, p.slim);
-  a.p[3] = weight_gradient(f, h, kblocks(T), dW2, 4, p.slim);
+  const Plan wp = weights_plan(T, h, f, pairs);
+  a.p[1] = weight_gradient(wp, h, f, kblocks(T), dW1, 2);
+  a.p[2] = weight_gradient(wp, h, f, kblocks(T), dW3, 3);
+  a.p[3] = weight_gradient(wp, f, h, kblocks(T), dW2, 4);
+  for (int i = 0; i < 4; ++i) {
+    a.p[i].planes = reinterpret_cast<float*>(planes);
+    planes += i ? plane_bytes(wp, f, h) : plane_bytes(p, T, h);
+  }
   a.np = 4;
   a.early = 1;
-  a.planes = planes;
   FFN_MAP(map_mn(&maps.a[0], W1, h, f));
   FFN_MAP(map_mn(&maps.a[1], W3, h, f));
   FFN_MAP(map_mn(&maps.a[2], x, h, T));
@@ -1008,18 +1065,19 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   FFN_MAP(map_mn(&maps.b[3], du, f, T));
   FFN_MAP(map_mn(&maps.b[4], dy, h, T));
   FFN_TRY("gradients launch", launch_gemm<kGrads>(maps, a, p.slim, pairs, st));
-  if (p.S > 1) FFN_TRY("join launch", launch_join(false, a, st));
+  FFN_TRY("join launch", launch_join(false, a, st));
   return MOE_OK;
 }
 
 int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]) {
-  if (T < 1 || pairs < 1 || !plan || launch < 0 || launch > 3 || check_block(T, h, f, MOE_BF16))
+  if (T < 1 || pairs < 1 || !plan || launch < 0 || launch > 4 || check_block(T, h, f, MOE_BF16))
     return set_error(MOE_ERR_INVALID_ARG, "bad launch, sizes or pairs");
   const Plan p = launch == 0   ? gu_plan(T, h, f, pairs)
                  : launch == 1 ? down_plan(T, h, f, pairs)
                  : launch == 2 ? dact_plan(T, h, f, pairs)
-                               : dx_plan(T, h, f, pairs);
-  const int kb = launch == 0 || launch == 2 ? kblocks(h) : kblocks(f) * (launch == 3 ? 2 : 1);
+                 : launch == 3 ? dx_plan(T, h, f, pairs)
+                               : weights_plan(T, h, f, pairs);
+  const int kb = launch == 4 ? kblocks(T) : launch == 0 || launch == 2 ? kblocks(h) : kblocks(f) * (launch == 3 ? 2 : 1);
   const int v[6] = {p.R, p.n_tile, p.S, p.mt, p.nt, kb};
   for (int i = 0; i < 6; ++i) plan[i] = v[i];
   return MOE_OK;

@@ -93,16 +93,20 @@ def test_tiles_cover_every_output(lib, h, f):
     out = (ctypes.c_int * 6)()
     for T in (1, 2, 15, 33, 64, 100, 128, 200, 256, 257, 400, 611, 1000, 1024, 2048, 5000, 8192, 100000):
         for pairs in (74, 66, 1):
-            for launch in range(4):
+            for launch in range(5):
                 assert lib.moe_test_ffn_plan(launch, T, h, f, pairs, out) == 0
                 R, n_tile, S, mt, nt, kb = list(out)
+                kbs = -(-kb // S)
+                assert 1 <= S <= 16 and (S - 1) * kbs < kb <= S * kbs
+                if launch == 4:
+                    assert R in (64, 128) and n_tile in (32, 64, 128, 256) and kb == -(-T // 64)
+                    assert S == 1 or pairs != 74 or lib.moe_ffn_backward_workspace(T, h, f) >= T * f * 4 + 3 * S * f * h * 4
+                    continue
                 M = f if launch in (0, 2) else h
                 unit = 2 if launch == 0 else 4
                 assert 8 <= R <= 128 and R % (64 if launch >= 2 else 8) == 0, (T, launch, list(out))
                 assert n_tile % 16 == 0 and 16 <= n_tile <= (128 if T <= 128 else 256)
                 assert (mt - 1) * unit * R < M <= mt * unit * R and (nt - 1) * n_tile < T <= nt * n_tile
-                kbs = -(-kb // S)
-                assert 1 <= S <= 16 and (S - 1) * kbs < kb <= S * kbs
                 if launch == 0:
                     assert S == 1  # the activation needs whole sums
                 # a stage of the pipeline fits, and so does what an MMA reads behind the last one
@@ -200,7 +204,8 @@ def check(got, want, dt, name):
 
 
 SIZES = [(1, 8, 8), (3, 64, 8), (2, 8, 200), (1, 128, 448), (100, 128, 448), (31, 72, 136), (33, 520, 264), (128, 1000, 2728),
-         (256, 256, 512), (257, 264, 520), (300, 2048, 4096), (611, 2040, 5464), (1025, 512, 1032), (2500, 136, 72)]
+         (256, 256, 512), (257, 264, 520), (300, 2048, 4096), (611, 2040, 5464), (1025, 512, 1032), (2500, 136, 72),
+         (5000, 64, 64), (8000, 128, 448), (3000, 256, 1032), (1500, 40, 520)]
 FEW = [(2, 4096, 14336), (3, 4096, 14336), (4, 40, 24), (5, 128, 448), (7, 4096, 14336), (8, 2040, 5464), (9, 1000, 2728),
        (16, 2048, 4096), (24, 264, 1032), (32, 1024, 2048), (33, 640, 1032), (50, 72, 1528), (64, 512, 1024), (64, 1528, 8),
        (40, 8, 1528), (12, 4096, 72), (6, 72, 14336),
