@@ -366,9 +366,10 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
         auto store_act = [&](const uint32_t* act, int c0) {  // R and M are even: both m of a lane's pair exist or neither
           store_cols<8>(act, reinterpret_cast<uint16_t*>(p.out) + (long long)(t.n0 + c0) * ld + m0, ld, c0, t.valid, in_m, lane);
         };
-        // with rounds of items to come the accumulators go back to the MMAs before the stores; slim launches have one
+        // with rounds of items to come the accumulators go back to the MMAs before the stores; slim launches have one, and
+        // there the loop stays a loop: instructions are fetched once a launch (1-4 % of the smallest calls)
         uint32_t act[SLIM ? 1 : kChunks][8];
-#pragma unroll
+#pragma unroll(SLIM ? 1 : kChunks)
         for (int i = 0; i < kChunks; ++i) {
           const int c0 = 16 * (group + kStride * i);
           if (c0 >= t.valid) continue;
