@@ -492,9 +492,14 @@ def _ffn_bytes(T: int, h: int, f: int, index: int):
             int(lib.moe_ffn_backward_workspace(T, h, f)))
 
 
+@functools.lru_cache(maxsize=256)
+def _saved_bytes(T: int, f: int) -> int:
+    return int(load_library().moe_ffn_saved_bytes(T, f))
+
+
 def ffn_saved(T: int, f: int, device) -> torch.Tensor:
     """A buffer for what ``ffn_forward`` saves for ``ffn_backward`` (``moe_ffn_saved_bytes``)."""
-    return torch.empty((int(load_library().moe_ffn_saved_bytes(T, f)),), dtype=torch.uint8, device=device)
+    return torch.empty((_saved_bytes(T, f),), dtype=torch.uint8, device=device)
 
 
 def ffn_forward(x, W1, W3, W2, residual=None, y=None, saved=None, stream=None):
