@@ -50,7 +50,9 @@ enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kGrads };
 // an SM each in shared memory, registers and tensor memory: with few tokens what counts is the gap between two launches,
 // and the next launch's CTAs set up and fetch their first weights beside the last ones of this launch.  Forward pass in
 // us, full form / slim form, tokens 64 and 128: (h 512, f 1024) 18.6 / 16.3, 18.1 / 16.8; (2048, 4096) 31.7 / 29.8, 32.9 /
-// 33.9; (4096, 4096) 48.8 / 46.5, 50.6 / 63.9; (4096, 14336) 76.6 / 75.8, 78.9 / 90.9.
+// 33.9; (4096, 4096) 48.8 / 46.5, 50.6 / 63.9; (4096, 14336) 76.6 / 75.8, 78.9 / 90.9.  Up to 32 columns a matrix of 96 MB and
+// more streams longer than the gap costs, and the full form has more of it in flight: 8 tokens of (4096, 14336) 67.2 /
+// 69.9, of (4096, 8192) 50.0 / 49.7.
 template <bool SLIM> struct Form {
   static constexpr int kEpiWarps = SLIM ? 4 : 16;
   static constexpr int kThreads = 96 + 32 * kEpiWarps;
@@ -671,6 +673,7 @@ Ring ring_of(int kind, int R, int n_tile, bool slim) {
 // a swizzle atom in part empty and cost 18 % (R 98 against 112, n_tile 256).
 bool is_slim(int kind, int M, int N, int KB) {
   if (kind == kGrads) return N <= Form<true>::kAccCols && (long long)M * KB * 32 <= (1 << 19);  // KB: of two segments
+  if (N <= 32 && (long long)M * KB * BK * 2 >= ((long long)96 << 20)) return false;
   return N <= 64 || (N <= Form<true>::kAccCols && KB <= 16);
 }
 

@@ -113,7 +113,7 @@ def test_tiles_cover_every_output(lib, h, f):
                 slot = -(-R // 64) * 8192 if launch >= 2 else -(-R // 8) * 1024
                 stage, tail = 2 * slot + n_tile * 64, max(0, 16384 - slot)
                 kept = 65536 if launch == 2 else 0  # of the da launch's epilogue; a fourth of it in the slim form
-                assert 1024 + tail + 2 * stage + kept <= 230400 and (T > 64 or 1024 + tail + 2 * stage + kept // 4 <= 114688)
+                assert 1024 + tail + 2 * stage + kept <= 230400 and (T > 64 or M * kb * 128 >= 96 << 20 or 1024 + tail + 2 * stage + kept // 4 <= 114688)
                 if S > 1:
                     ws = lib.moe_ffn_forward_workspace if launch == 1 else lib.moe_ffn_backward_workspace
                     if pairs == 74:  # without a device the library assumes 148 multiprocessors
