@@ -477,7 +477,7 @@ def _add_rmsnorm_backward(index, st, d_out, s, rstd, gain, d_s, dx, dgain):
     wp, n = None, 0
     if dgain is not None:
         n = _norm_workspace(T, h, index)
-        ws = d_out.new_empty((n,), dtype=torch.uint8)
+        ws = d_out.new_empty(n, dtype=torch.uint8)
         wp = ws.data_ptr()
     _check(load_library().moe_add_rmsnorm_backward(d_out.data_ptr(), ep, sp, tp, gp, T, h, DTYPES[dt], xp,
                                                    _operand("dgain", dgain, dt, (h,), index), wp, n, st))
@@ -499,7 +499,7 @@ def _saved_bytes(T: int, f: int) -> int:
 
 def ffn_saved(T: int, f: int, device) -> torch.Tensor:
     """A buffer for what ``ffn_forward`` saves for ``ffn_backward`` (``moe_ffn_saved_bytes``)."""
-    return torch.empty((_saved_bytes(T, f),), dtype=torch.uint8, device=device)
+    return torch.empty(_saved_bytes(T, f), dtype=torch.uint8, device=device)
 
 
 def ffn_forward(x, W1, W3, W2, residual=None, y=None, saved=None, stream=None):
@@ -524,7 +524,7 @@ def _ffn_forward(index, st, x, W1, W3, W2, residual, y, saved):
     n_saved, n, _ = _ffn_bytes(T, h, f, index)
     sp = _operand("saved", saved, torch.uint8, (n_saved,), index)
     yp, y = _output("y", y, x, index)
-    ws = x.new_empty((n,), dtype=torch.uint8)
+    ws = x.new_empty(n, dtype=torch.uint8)
     _check(load_library().moe_ffn_forward(x.data_ptr(), w1, w3, w2, rp, T, h, f, DTYPES[dt], yp, sp, ws.data_ptr(), n, st))
     return y
 
@@ -544,7 +544,7 @@ def _ffn_backward(index, st, d_y, x, W1, W3, W2, saved, dx, dW1, dW3, dW2):
     w2, sp = _operand("W2", W2, dt, (h, f), index), _operand("saved", saved, torch.uint8, (n_saved,), index)
     (xp, dx), (p1, dW1) = _output("dx", dx, x, index), _output("dW1", dW1, W1, index)
     (p3, dW3), (p2, dW2) = _output("dW3", dW3, W3, index), _output("dW2", dW2, W2, index)
-    ws = x.new_empty((n,), dtype=torch.uint8)
+    ws = x.new_empty(n, dtype=torch.uint8)
     _check(load_library().moe_ffn_backward(dp, x.data_ptr(), w1, w3, w2, sp, T, h, f, DTYPES[dt], xp, p1, p3, p2,
                                            ws.data_ptr(), n, st))
     return dx, dW1, dW3, dW2
