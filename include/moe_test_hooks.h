@@ -73,6 +73,15 @@ void moe_test_set_free_bytes_limit(long long bytes);
 int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]);
 
 /*
+ * Host side only.  Items that a pair of multiprocessors gets in the launch of the block's gradients
+ * on a machine of `pairs` pairs (the launch has no more pairs than items): items receives the first
+ * `most` of them in their order, deal[3] how many the launch has, how many the pair, and the one of
+ * which the pair reads operands before the launch in front is complete (-1: none).
+ * Errors: MOE_ERR_INVALID_ARG.
+ */
+int moe_test_ffn_deal(int T, int h, int f, int pairs, int pair, int* items, int most, int deal[3]);
+
+/*
  * The wait of moe_test_wait_expiry_pair (its leader) on the given stream, reported where the
  * feed-forward block's kernels report theirs: the next moe_operators_status returns
  * MOE_ERR_DEVICE_TIMEOUT once.  Errors: MOE_ERR_INVALID_ARG, MOE_ERR_ARCH, MOE_ERR_CUDA.

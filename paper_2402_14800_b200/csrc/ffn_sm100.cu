@@ -158,11 +158,19 @@ struct Item {
 
 // The k-th item of a pair, past the last one when there is none.  Items are dealt in rounds; where dx shares a launch
 // with the weights' gradients the pairs that got one of its long items join the rounds of short ones late.
-template <int KIND> __device__ __forceinline__ int item_of(const Args& a, int k, int pair, int n_pairs) {
+template <int KIND> __host__ __device__ __forceinline__ int item_of(const Args& a, int k, int pair, int n_pairs) {
   if (KIND != kGrads || a.first == 0) return pair + k * n_pairs;
   const int rest = n_pairs - a.first;
   if (pair < a.first) return k == 0 ? pair : a.first + a.skip * rest + (k - 1) * n_pairs + pair;
   return a.first + (k < a.skip ? k * rest + pair - a.first : a.skip * rest + (k - a.skip) * n_pairs + pair);
+}
+
+// The item of which a pair may read A ahead of the wait, -1 for none.  There are at least as many items as pairs, but a
+// pair can have none all the same: without a round that is left out (skip 0) the pairs of dx take part in the first round
+// of the others, and the last pairs find it empty.  What such a pair loaded would still be under way when its CTAs end.
+template <int KIND> __host__ __device__ __forceinline__ int item_ahead(const Args& a, int pair, int n_pairs, int n_items) {
+  const int item = item_of<KIND>(a, 0, pair, n_pairs);
+  return a.early && item < n_items ? item : -1;
 }
 
 // Items of a problem: k-split -> band of at most kBandTiles n tiles -> m tile -> n tile, so that the items in
@@ -283,8 +291,9 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
     // The launch before this one let it start after its own wait (below), so everything older than that launch is
     // complete, the weights among it: the first ring of stages of A may come before the wait.
     uint32_t ahead = 0;
-    if (args.early && pair < n_items) {
-      const Item t = decode_item<KIND>(args, item_of<KIND>(args, 0, pair, n_pairs));
+    const int early = item_ahead<KIND>(args, pair, n_pairs, n_items);
+    if (early >= 0) {
+      const Item t = decode_item<KIND>(args, early);
       ahead = min(ns, (uint32_t)(t.kb1 - t.kb0));
       if (lane == 0)
         for (uint32_t i = 0; i < ahead; ++i) load_a(t, t.kb0 + (int)i, i);
@@ -765,20 +774,15 @@ Plan choose_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
-  const Ring ring = ring_of(KIND, a.p[0].R, a.p[0].n_tile, SLIM);
-  a.slot_a = ring.slot_a;
-  a.stage = ring.stage;
-  a.tail = ring.tail;
-  int items = 0, kbs = 2;
+// Splits the contractions and deals the items; returns how many there are.
+int deal_items(int kind, Args& a, int pairs) {
+  int items = 0;
   for (int i = 0; i < a.np; ++i) {
     Problem& p = a.p[i];
     p.kbs = (p.KB + p.S - 1) / p.S;
-    kbs = std::max(kbs, p.kbs);
     items += p.mt * p.nt * p.S;
   }
-  a.stages = std::min(ring.stages, kbs);
-  if (KIND == kGrads) {
+  if (kind == kGrads) {
     // an item of dx against one of the weights' gradients, in cycles: the tensor pipe, or what a pair draws of weights
     // (600 a k-block) and stores (9000 an item)
     const Problem &x = a.p[0], &w = a.p[1];
@@ -786,6 +790,18 @@ template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a
     a.first = n < grid ? n : 0;
     a.skip = a.first ? (int)(x.kbs * std::max(4.6 * x.n_tile, 600.0) / std::max(std::max(4.6 * w.n_tile, 800.0) * w.kbs + 4000.0, 9000.0)) : 0;
   }
+  return items;
+}
+
+template <int KIND, bool SLIM> cudaError_t launch_form(const Maps& maps, Args& a, int pairs, cudaStream_t st) {
+  const Ring ring = ring_of(KIND, a.p[0].R, a.p[0].n_tile, SLIM);
+  a.slot_a = ring.slot_a;
+  a.stage = ring.stage;
+  a.tail = ring.tail;
+  const int items = deal_items(KIND, a, pairs);
+  int kbs = 2;
+  for (int i = 0; i < a.np; ++i) kbs = std::max(kbs, a.p[i].kbs);
+  a.stages = std::min(ring.stages, kbs);
   static std::atomic<unsigned long long> set{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -868,6 +884,19 @@ Plan dx_plan(int T, int h, int f, int pairs) { return choose_plan(kGrads, h, T, 
 Plan weights_plan(int T, int h, int f, int pairs) {
   const bool slim = dx_plan(T, h, f, pairs).slim;  // one launch, one form
   return choose_plan(slim ? -2 : -1, h, T, f, slim, pairs);
+}
+
+// The gradients' launch but for its operands and outputs.
+Args grads_args(int T, int h, int f, int dtype, int pairs) {
+  Args a = args_of(problem_of(dx_plan(T, h, f, pairs), h, T, 2 * kblocks(f), nullptr), dtype);
+  a.p[0].segKB = kblocks(f);
+  const Plan wp = weights_plan(T, h, f, pairs);
+  a.p[1] = weight_gradient(wp, h, f, kblocks(T), nullptr, 2);
+  a.p[2] = weight_gradient(wp, h, f, kblocks(T), nullptr, 3);
+  a.p[3] = weight_gradient(wp, f, h, kblocks(T), nullptr, 4);
+  a.np = 4;
+  a.early = 1;
+  return a;
 }
 
 // the saved buffer: (p, q), then a
@@ -1046,18 +1075,13 @@ int moe_ffn_backward(const void* dy, const void* x, const void* W1, const void* 
   FFN_TRY("join launch", launch_join(true, a, st));
   // dx = dg W1 + du W3; dW1 = dg^T x, dW3 = du^T x (rows f, contiguous h), dW2 = dy^T a (rows h, contiguous f)
   p = dx_plan(T, h, f, pairs);
-  a = args_of(problem_of(p, h, T, 2 * kblocks(f), dx), dtype);
-  a.p[0].segKB = kblocks(f);
-  const Plan wp = weights_plan(T, h, f, pairs);
-  a.p[1] = weight_gradient(wp, h, f, kblocks(T), dW1, 2);
-  a.p[2] = weight_gradient(wp, h, f, kblocks(T), dW3, 3);
-  a.p[3] = weight_gradient(wp, f, h, kblocks(T), dW2, 4);
+  a = grads_args(T, h, f, dtype, pairs);
+  void* grads[4] = {dx, dW1, dW3, dW2};
   for (int i = 0; i < 4; ++i) {
+    a.p[i].out = grads[i];
     a.p[i].planes = reinterpret_cast<float*>(planes);
-    planes += i ? plane_bytes(wp, f, h) : plane_bytes(p, T, h);
+    planes += i ? plane_bytes(weights_plan(T, h, f, pairs), f, h) : plane_bytes(p, T, h);
   }
-  a.np = 4;
-  a.early = 1;
   FFN_MAP(map_mn(&maps.a[0], W1, h, f));
   FFN_MAP(map_mn(&maps.a[1], W3, h, f));
   FFN_MAP(map_mn(&maps.a[2], x, h, T));
@@ -1084,6 +1108,21 @@ int moe_test_ffn_plan(int launch, int T, int h, int f, int pairs, int plan[6]) {
   const int kb = launch == 4 ? kblocks(T) : launch == 0 || launch == 2 ? kblocks(h) : kblocks(f) * (launch == 3 ? 2 : 1);
   const int v[6] = {p.R, p.n_tile, p.S, p.mt, p.nt, kb};
   for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  return MOE_OK;
+}
+
+int moe_test_ffn_deal(int T, int h, int f, int pairs, int pair, int* items, int most, int deal[3]) {
+  if (T < 1 || pairs < 1 || !items || !deal || most < 0 || check_block(T, h, f, MOE_BF16))
+    return set_error(MOE_ERR_INVALID_ARG, "bad sizes or pairs");
+  Args a = grads_args(T, h, f, MOE_BF16, pairs);
+  const int total = deal_items(kGrads, a, pairs), grid = std::min(total, pairs);
+  if (pair < 0 || pair >= grid) return set_error(MOE_ERR_INVALID_ARG, "pair = %d of %d", pair, grid);
+  int n = 0;
+  for (int item; (item = item_of<kGrads>(a, n, pair, grid)) < total; ++n)
+    if (n < most) items[n] = item;
+  deal[0] = total;
+  deal[1] = n;
+  deal[2] = item_ahead<kGrads>(a, pair, grid, total);
   return MOE_OK;
 }
 
