@@ -705,8 +705,9 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
   if (dgain && (!workspace || workspace_bytes < moe_add_rmsnorm_backward_workspace(T, h)))
     return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0,
                      moe_add_rmsnorm_backward_workspace(T, h));
-  // dx may be d_s (each element is read before it is written), but the other operands are read again by the gain's sums
-  if (overlap(dx, n, d_out, n) || overlap(dx, n, s, n) || (dx != d_s && overlap(dx, n, d_s, n)))
+  // dx may be d_s (each element is read before it is written), but the other operands are read again: d_out and s by the
+  // gain's sums, the gain by blocks that start later and for every row that the registers do not hold
+  if (overlap(dx, n, d_out, n) || overlap(dx, n, s, n) || overlap(dx, n, gain, h * e) || (dx != d_s && overlap(dx, n, d_s, n)))
     return set_error(MOE_ERR_INVALID_ARG, "dx overlaps an input (only d_s itself is allowed)");
   if (overlap(dgain, h * e, d_out, n) || overlap(dgain, h * e, s, n) || overlap(dgain, h * e, dx, n) ||
       overlap(dgain, h * e, gain, h * e) || overlap(dgain, h * e, d_s, n))

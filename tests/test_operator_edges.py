@@ -36,3 +36,26 @@ def test_gradients_launch_deals_each_item_once_and_reads_ahead_only_for_an_item(
                 seen += mine
             assert sorted(seen) == list(range(total)), (T, pairs)
     assert lib.moe_test_ffn_deal(1, 8, 8, 74, 4, items, most, deal) == -1  # four items: the launch has four pairs
+
+
+def test_norm_gradients_refuse_every_overlap_with_an_output(lib):
+    """Each output against each other tensor, at the same address and in part; dx may only be d_s itself."""
+    T, h, e = 64, 256, 2
+    n, g, r, w = T * h * e, h * e, T * 4, lib.moe_add_rmsnorm_backward_workspace(64, 256)
+    names = ("d_out", "d_s", "s", "rstd", "gain", "dx", "dgain", "workspace")
+    size = dict(zip(names, (n, n, n, r, g, n, g, w)))
+    at = {k: (i + 1) << 28 for i, k in enumerate(names)}
+
+    def call(**moved):
+        a = {k: ctypes.c_void_p({**at, **moved}[k]) for k in names}
+        return lib.moe_add_rmsnorm_backward(a["d_out"], a["d_s"], a["s"], a["rstd"], a["gain"], T, h, 0, a["dx"], a["dgain"],
+                                            a["workspace"], w, None)
+
+    for out in ("dx", "dgain", "workspace"):
+        for other in names:
+            if other == out:
+                continue
+            for place in (at[other], at[other] + size[other] - 16, at[other] - size[out] + 16):
+                if (out, other) == ("dx", "d_s") and place == at[other]:
+                    continue
+                assert call(**{out: place}) == -1 and "overlap" in binding.last_error(), (out, other, place - at[other])
