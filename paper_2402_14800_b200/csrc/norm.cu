@@ -634,6 +634,7 @@ int forward(const void* x, const void* residual, const void* gain, int T, int h,
     return set_error(MOE_ERR_INVALID_ARG, "residual and s go together: both or neither");
   if (!aligned16(x) || !aligned16(residual) || !aligned16(gain) || !aligned16(out) || !aligned16(s))
     return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  if (!aligned4(rstd) || !aligned4(scales)) return set_error(MOE_ERR_INVALID_ARG, "rstd or scales is not aligned to its fp32 values");
   const size_t e = (size_t)element_size(dtype), n = (size_t)T * h * e;
   const size_t n_out = q ? (size_t)T * h : n;
   // an output may be an input of the same place and type (its row is read before it is written), nothing in between
@@ -702,6 +703,7 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
   if (!d_out || !s || !rstd || !dx) return set_error(MOE_ERR_INVALID_ARG, "d_out, s, rstd or dx is NULL");
   if (!aligned16(d_out) || !aligned16(d_s) || !aligned16(s) || !aligned16(gain) || !aligned16(dx))
     return set_error(MOE_ERR_INVALID_ARG, "every tensor must be 16-byte aligned");
+  if (!aligned4(rstd)) return set_error(MOE_ERR_INVALID_ARG, "rstd is not aligned to its fp32 values");
   if (dgain && (!workspace || workspace_bytes < moe_add_rmsnorm_backward_workspace(T, h)))
     return set_error(MOE_ERR_INVALID_ARG, "workspace of %zu bytes, %zu are needed", workspace ? workspace_bytes : (size_t)0,
                      moe_add_rmsnorm_backward_workspace(T, h));

@@ -19,6 +19,7 @@ inline int sm_count() {
   return n[dev];
 }
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // [p, p + n) against [q, q + m); a null pointer overlaps nothing

@@ -59,3 +59,15 @@ def test_norm_gradients_refuse_every_overlap_with_an_output(lib):
                 if (out, other) == ("dx", "d_s") and place == at[other]:
                     continue
                 assert call(**{out: place}) == -1 and "overlap" in binding.last_error(), (out, other, place - at[other])
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_norm_refuses_fp32_buffers_between_two_values(lib, off):
+    p = [ctypes.c_void_p(0x100000 * (i + 1)) for i in range(8)]
+    astray = ctypes.c_void_p(0x800000 + off)
+    assert lib.moe_add_rmsnorm(p[0], p[1], p[2], 4, 64, 1e-5, 0, p[3], p[4], astray, None) == -1
+    assert "aligned" in binding.last_error()
+    assert lib.moe_add_rmsnorm_e4m3(p[0], p[1], p[2], 4, 64, 1e-5, 0, 0, p[3], astray, p[4], None) == -1
+    assert "aligned" in binding.last_error()
+    assert lib.moe_add_rmsnorm_backward(p[0], p[1], p[2], astray, p[3], 4, 64, 0, p[4], p[5], p[6], 1 << 20, None) == -1
+    assert "aligned" in binding.last_error()
