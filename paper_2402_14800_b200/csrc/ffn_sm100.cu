@@ -643,6 +643,10 @@ struct Plan {
   bool slim;
 };
 
+// The kernel counts items in 32 bits, those of up to four problems together.  The largest sizes that the calls take, 2^24
+// tokens of 2^20 by 2^20, are 2^28 items of the largest tile; small tiles of them would be 2^32 and more.
+constexpr long long kMostItems = 1 << 29;
+
 // Pipeline of a tile: bytes of an accumulator's rows of A and of a stage, and the stages that fit.
 struct Ring {
   int slot_a, stage, tail, stages;
@@ -696,23 +700,25 @@ Plan search_plan(int kind, int M, int N, int KB, bool may_split, int pairs) {
     const int nt = (N + cols - 1) / cols;
     const int n_tile = ((N + nt - 1) / nt + 15) / 16 * 16;
     if (n_tile != cols) continue;  // the same tiles with fewer columns come later
-    for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4 && (S - 1) * nt * mt_min < 2 * pairs)); ++S) {
+    for (int S = 1; S <= 16 && (S == 1 || (may_split && KB / S >= 4 && (long long)(S - 1) * nt * mt_min < 2 * pairs)); ++S) {
       const int kbs = (KB + S - 1) / S;
       if ((KB + kbs - 1) / kbs != S) continue;
-      const int least = (mt_min * nt * S + pairs - 1) / pairs;
+      const long long least = ((long long)mt_min * nt * S + pairs - 1) / pairs;  // rounds
       for (int fill = 0; fill < 2; ++fill) {  // whole tiles, or as many rows as fill the rounds
         int R = kAccRows;
         if (fill) {
           if (a_mn(kind)) {
             R = 64;
           } else {
-            const int most = least * pairs / (nt * S);
-            R = ((M + unit * most - 1) / (unit * most) + 7) / 8 * 8;
+            const long long most = least * pairs / (nt * S);
+            R = (int)((M + unit * most - 1) / (unit * most) + 7) / 8 * 8;
           }
           if (R >= kAccRows) continue;
         }
         const int mt = (M + unit * R - 1) / (unit * R);
-        const int items = mt * nt * S, full = items / pairs, rest = items - full * pairs;
+        const long long items = (long long)mt * nt * S, full = items / pairs;
+        const int rest = (int)(items - full * pairs);
+        if (items > kMostItems) continue;
         const int stages = ring_of(kind, R, n_tile, slim).stages;
         auto round = [&](int active) {
           const double l2 = active * (4.0 * R + n_tile) * 128 / 7600.0;
@@ -746,7 +752,7 @@ Plan search_weights_plan(int T, int h, int f, int pairs, bool slim) {
         if ((KB + kbs - 1) / kbs != S) continue;
         auto tiles = [&](int M, int N) { return (long long)((M + 4 * R - 1) / (4 * R)) * ((N + n - 1) / n); };
         const long long items = S * (2 * tiles(h, f) + tiles(f, h));
-        if (S > 1 && items > 4 * pairs) break;
+        if ((S > 1 && items > 4 * pairs) || items > kMostItems) break;
         double cost = (double)((items + pairs - 1) / pairs) * (kbs * std::max(800.0, 4.6 * n) + 2000.0 + 8.0 * n);
         if (S > 1) cost += 4500.0 + 3.0 * S * h * f * 8 / 7000.0;
         if (cost < best_cost) {

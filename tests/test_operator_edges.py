@@ -71,3 +71,34 @@ def test_norm_refuses_fp32_buffers_between_two_values(lib, off):
     assert "aligned" in binding.last_error()
     assert lib.moe_add_rmsnorm_backward(p[0], p[1], p[2], astray, p[3], 4, 64, 0, p[4], p[5], p[6], 1 << 20, None) == -1
     assert "aligned" in binding.last_error()
+
+
+LARGEST = """
+import ctypes
+from paper_2402_14800_b200 import binding
+lib = binding.load_library()
+out = (ctypes.c_int * 6)()
+for T in ((1 << 24) - 5, 1 << 24):
+    for h, f in ((8, 1 << 20), (1 << 20, 8), (1 << 20, 1 << 20), (4096, 1 << 20)):
+        for pairs in (74, 1):
+            for launch in range(4):
+                assert lib.moe_test_ffn_plan(launch, T, h, f, pairs, out) == 0
+                R, n_tile, S, mt, nt, kb = list(out)
+                M, unit = f if launch in (0, 2) else h, 2 if launch == 0 else 4
+                assert 8 <= R <= 128 and 16 <= n_tile <= 256 and 1 <= S <= 16
+                assert (mt - 1) * unit * R < M <= mt * unit * R and (nt - 1) * n_tile < T <= nt * n_tile
+                assert mt * nt * S <= 1 << 29
+        assert lib.moe_ffn_forward_workspace(T, h, f) >= 2 * T * f and lib.moe_ffn_backward_workspace(T, h, f) >= 4 * T * f
+        assert lib.moe_ffn_saved_bytes(T, f) >= 10 * T * f
+print("planned")
+"""
+
+
+def test_the_largest_sizes_have_plans(lib):
+    """Sizes that pass the argument check but no memory: what asks for a workspace or a plan still gets an answer."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", LARGEST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "planned" in r.stdout, (r.returncode, r.stdout + r.stderr)
