@@ -88,6 +88,12 @@ int moe_test_ffn_deal(int T, int h, int f, int pairs, int pair, int* items, int 
  */
 int moe_test_operators_expiry(unsigned limit_us, void* cuda_stream);
 
+/*
+ * A launch of one thread that lets the stream's next launch start at once, as the norm's kernels
+ * do, and takes `ms` milliseconds itself.  Errors: MOE_ERR_INVALID_ARG (beyond 1..6000), MOE_ERR_CUDA.
+ */
+int moe_test_hold(unsigned ms, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

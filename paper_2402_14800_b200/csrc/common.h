@@ -118,7 +118,17 @@ struct KeptIds {
 // predecessor wrote (or still reads).  Every kernel on the forward path calls
 // pdl_launch_dependents() and pdl_wait() first thing (the GEMMs after their set-up), so the
 // stream order of all memory accesses is unchanged and only launch latency and prologues overlap.
-// The one exception are the down launches of gemm_pair_n, gemm_weights_m and gemm_tokens_d: before they wait they
+//
+// Two groups of launches read ahead of their wait.
+//
+// The dense block's: the down launch (ffn_gemm_kernel with `early`, ffn_gemv_down_kernel, ffn_mma_kernel) fetches W2, the
+// launch of the gradients W1, W3, x and the saved a.  The launch directly before each of them is of the same call
+// (gate/up; da or the join behind it) and triggers behind its own wait, so whatever is older than that launch is complete,
+// and it writes none of these.  A kernel that triggers ahead of its wait, as all of norm.cu do, may not stand directly
+// before such a launch.  All warps of ffn_gemm_kernel that wait for data pass pdl_wait() first: the limit of their
+// waits counts the launch's own time.
+//
+// The down launches of gemm_pair_n, gemm_weights_m and gemm_tokens_d: before they wait they
 // read the batch description (Meta) and fetch weights (handover_wait in gemm_sm100.cu), and their MMA warps never wait.
 // What that rests on: Meta is complete before the gate/up launch of the batch passes its own wait, and that launch
 // triggers only then.  So nothing from the gate/up launch to the last down launch of a batch (the combine kernels between

@@ -316,8 +316,11 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
     }
     issued = max(issued, ahead);
   } else if (warp <= 2) {
-    // ---- MMA issuers of the leader, one warp per accumulator
+    // ---- MMA issuers of the leader, one warp per accumulator.  No stage is full before the producers have passed the
+    // wait; these warps pass it too, so that the limit of their first wait counts this launch's time and not what is left
+    // of a launch in front that let this one start at once.
     if (rank == 0) {
+      pdl_wait();
       const uint32_t acc = (uint32_t)warp - 1u;
       const uint32_t d_tmem = tmem_base + (uint32_t)kAccCols * acc;
       const uint32_t tmem_full = smem_u32(&bars.tmem_full[acc]), tmem_empty = smem_u32(&bars.tmem_empty[acc]);
@@ -589,6 +592,12 @@ ffn_gemm_kernel(const __grid_constant__ Maps maps, const Args args) {
   }
 
   teardown_pair(bars, tmem_base, 2 * kAccCols, issued, ns, rank, &g_status);
+}
+
+// Lets its successor start at once and takes `ns` itself (moe_test_hold).
+__global__ void hold_kernel(unsigned long long ns) {
+  pdl_launch_dependents();
+  for (const unsigned long long t0 = gtimer(); gtimer() - t0 < ns;) __nanosleep(1000);
 }
 
 // Sum of the S planes of a split launch in their order, and what the epilogue would have done with it: four
@@ -1140,6 +1149,12 @@ int moe_test_operators_expiry(unsigned limit_us, void* cuda_stream) {
   FFN_TRY("the status word's address", cudaGetSymbolAddress(&status, g_status));
   FFN_TRY("launch", launch_wait_expiry_pair(static_cast<int*>(status), (unsigned long long)limit_us * 1000ull, 0,
                                             static_cast<cudaStream_t>(cuda_stream)));
+  return MOE_OK;
+}
+
+int moe_test_hold(unsigned ms, void* cuda_stream) {
+  if (ms < 1 || ms > 6000) return set_error(MOE_ERR_INVALID_ARG, "ms = %u outside 1..6000", ms);
+  FFN_TRY("launch", launch_plain(hold_kernel, dim3(1), dim3(1), 0, static_cast<cudaStream_t>(cuda_stream), ms * 1000000ull));
   return MOE_OK;
 }
 

@@ -102,3 +102,37 @@ def test_the_largest_sizes_have_plans(lib):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", LARGEST], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "planned" in r.stdout, (r.returncode, r.stdout + r.stderr)
+
+
+# ------------------------------------------------------------------------------- on the device
+
+
+def block_inputs(T, h, f, dt, seed=0):
+    g = torch.Generator(DEV).manual_seed(seed)
+
+    def normal(*shape, std=1.0):
+        return (torch.randn(shape, generator=g, device=DEV) * std).to(dt)
+
+    return (normal(T, h), normal(f, h, std=1.28 / h ** 0.5), normal(f, h, std=1.28 / h ** 0.5), normal(h, f, std=1.28 / f ** 0.5),
+            normal(T, h, std=0.1))
+
+
+@gpu
+@pytest.mark.parametrize("T", [40, 300])
+def test_a_long_launch_in_front_does_not_count_against_the_waits(lib, T):
+    """The kernels' waits give up after 4 s; a launch in front that lets them start at once may take longer."""
+    h, f = 520, 1032
+    x, W1, W3, W2, dy = block_inputs(T, h, f, torch.bfloat16, seed=2)
+
+    def step():
+        saved = binding.ffn_saved(T, f, DEV)
+        y = binding.ffn_forward(x, W1, W3, W2, saved=saved)
+        return y, *binding.ffn_backward(dy, x, W1, W3, W2, saved)
+
+    want = step()
+    assert binding.operators_status(DEV) == 0
+    assert lib.moe_test_hold(0, None) == -1 and lib.moe_test_hold(6001, None) == -1
+    assert lib.moe_test_hold(4600, torch.cuda.current_stream().cuda_stream) == 0
+    got = step()
+    assert binding.operators_status(DEV) == 0
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
