@@ -94,6 +94,12 @@ int moe_test_operators_expiry(unsigned limit_us, void* cuda_stream);
  */
 int moe_test_hold(unsigned ms, void* cuda_stream);
 
+/*
+ * The next `times` times that the norm's kernels ask how many of their blocks an SM holds (once a
+ * kernel and device), the question fails.  Errors: MOE_ERR_INVALID_ARG.
+ */
+int moe_test_fail_occupancy(int times);
+
 #ifdef __cplusplus
 }
 #endif

@@ -101,6 +101,7 @@ def load_library(path: str | None = None):
     lib.moe_test_host_slabs.argtypes = [vp, ci]
     lib.moe_test_operators_expiry.argtypes = [ctypes.c_uint, vp]
     lib.moe_test_hold.argtypes = [ctypes.c_uint, vp]
+    lib.moe_test_fail_occupancy.argtypes = [ci]
     lib.moe_test_ffn_plan.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(ci)]
     lib.moe_test_ffn_deal.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(ci), ci, ctypes.POINTER(ci)]
     lib.moe_test_set_free_bytes_limit.restype = None

@@ -19,6 +19,7 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include "moe_test_hooks.h"
 #include "operators.h"
 
 namespace moe {
@@ -539,24 +540,44 @@ Cut cut_of(int h, int E, bool forward) {
   return {256, 0};
 }
 
-// Blocks of a persistent launch: what is resident at once, so that every block walks about as many rows.
+std::atomic<int> g_fail_occupancy{0};  // moe_test_fail_occupancy
+
+// Blocks of a persistent launch: what is resident at once, so that every block walks about as many rows.  A kernel's
+// blocks per SM are asked for once a device and remembered when there was an answer.
 constexpr int kBlocksPerSm = 8;  // of the backward pass at most: partial sums of the gain's gradient are sized for it
-template <typename... KArgs> int grid_of(void (*kernel)(KArgs...), int T, const Cut& c, int most_blocks, int* cached) {
+struct Resident {
+  std::atomic<int> blocks[64];
+};
+template <typename... KArgs>
+cudaError_t grid_of(void (*kernel)(KArgs...), int T, const Cut& c, int most_blocks, Resident& known, int* grid) {
   const int threads = c.tpr == 32 ? 256 : c.tpr, rows = threads / c.tpr;
-  if (!*cached) {
-    int n = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != cudaSuccess || n < 1) n = 1;
-    *cached = n < most_blocks ? n : most_blocks;
+  int dev = 0, n = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64) n = known.blocks[dev].load(std::memory_order_relaxed);
+  if (!n) {
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0);
+    if (g_fail_occupancy.load(std::memory_order_relaxed) > 0) {
+      g_fail_occupancy.fetch_sub(1);
+      e = cudaErrorUnknown;
+    }
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorInvalidConfiguration;
+    n = n < most_blocks ? n : most_blocks;
+    if (dev < 64) known.blocks[dev].store(n, std::memory_order_relaxed);
   }
-  const int need = (T + rows - 1) / rows, most = sm_count() * *cached;
-  return need < most ? need : most;
+  const int need = (T + rows - 1) / rows, most = sm_count() * n;
+  *grid = need < most ? need : most;
+  return cudaSuccess;
 }
 
 #define MOE_NORM_CUTS(CASE) CASE(32, 1) CASE(32, 2) CASE(32, 4) CASE(256, 1) CASE(256, 2) CASE(256, 4)
 
 template <typename T, int E, int TPR, int NV, bool Q> cudaError_t launch_norm_cut(const NormArgs& a, cudaStream_t st) {
-  static int blocks = 0;
-  const int grid = grid_of(add_rmsnorm_kernel<T, E, TPR, NV, Q>, a.T, {TPR, NV}, 16, &blocks);
+  static Resident known = {};
+  int grid = 0;
+  const cudaError_t e = grid_of(add_rmsnorm_kernel<T, E, TPR, NV, Q>, a.T, {TPR, NV}, 16, known, &grid);
+  if (e != cudaSuccess) return e;
   return launch_pdl(add_rmsnorm_kernel<T, E, TPR, NV, Q>, dim3(grid), dim3(Shape<TPR>::kThreads), 0, st, a);
 }
 
@@ -577,8 +598,9 @@ template <typename T> cudaError_t launch_norm_type(const NormArgs& a, bool q, cu
 }
 
 template <typename T, int E, int TPR, int NV> cudaError_t launch_bwd_cut(const NormBwdArgs& a, int* grid, cudaStream_t st) {
-  static int blocks = 0;
-  *grid = grid_of(add_rmsnorm_backward_kernel<T, E, TPR, NV>, a.T, {TPR, NV}, kBlocksPerSm, &blocks);
+  static Resident known = {};
+  const cudaError_t e = grid_of(add_rmsnorm_backward_kernel<T, E, TPR, NV>, a.T, {TPR, NV}, kBlocksPerSm, known, grid);
+  if (e != cudaSuccess) return e;
   return launch_pdl(add_rmsnorm_backward_kernel<T, E, TPR, NV>, dim3(*grid), dim3(Shape<TPR>::kThreads), 0, st, a);
 }
 
@@ -726,6 +748,12 @@ int moe_add_rmsnorm_backward(const void* d_out, const void* d_s, const void* s, 
                           : dtype == MOE_FP16 ? launch_bwd_type<__half>(a, dgain, partial, st)
                                               : launch_bwd_type<float>(a, dgain, partial, st);
   if (err != cudaSuccess) return set_error(MOE_ERR_CUDA, "add_rmsnorm_backward launch: %s", cudaGetErrorString(err));
+  return MOE_OK;
+}
+
+int moe_test_fail_occupancy(int times) {
+  if (times < 0) return set_error(MOE_ERR_INVALID_ARG, "times = %d", times);
+  g_fail_occupancy.store(times);
   return MOE_OK;
 }
 

@@ -1,22 +1,23 @@
 // Host-side checks that the operators on the caller's own tensors share (norm.cu, ffn_sm100.cu).
 #pragma once
 
+#include <atomic>
+
 #include "common.h"
 
 namespace moe {
 
 constexpr int kMaxOperatorTokens = 1 << 24;
 
-// Multiprocessors of the current device.
+// Multiprocessors of the current device; 148 where there is none to ask.
 inline int sm_count() {
-  static int n[64] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (!n[dev]) {
-    int v = 0;
-    n[dev] = cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && v > 0 ? v : 148;
-  }
-  return n[dev];
+  static std::atomic<int> known[64] = {};
+  int dev = 0, v = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 148;
+  if (dev < 64 && (v = known[dev].load(std::memory_order_relaxed))) return v;
+  if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1) return 148;
+  if (dev < 64) known[dev].store(v, std::memory_order_relaxed);
+  return v;
 }
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }

@@ -136,3 +136,43 @@ def test_a_long_launch_in_front_does_not_count_against_the_waits(lib, T):
     got = step()
     assert binding.operators_status(DEV) == 0
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+FAILED_QUESTION = """
+import torch
+from paper_2402_14800_b200 import binding
+lib = binding.load_library()
+x, gain = torch.randn((700, 1024), device="cuda").bfloat16(), torch.ones(1024, device="cuda").bfloat16()
+rstd = torch.empty(700, device="cuda")
+
+def forward():
+    return binding.add_rmsnorm(x, x, gain, rstd=rstd)
+
+def e4m3():
+    return binding.add_rmsnorm_e4m3(x, x, gain)
+
+def backward():
+    return binding.add_rmsnorm_backward(x, x, torch.ones(700, device="cuda"), gain)
+
+for call in (forward, e4m3, backward):
+    assert lib.moe_test_fail_occupancy(1) == 0
+    try:
+        call()
+        raise SystemExit("%s went on after a failed question" % call.__name__)
+    except binding.MoeError as e:
+        assert "unknown error" in str(e), e
+    assert lib.moe_test_fail_occupancy(0) == 0
+    call()
+torch.cuda.synchronize()
+print("asked again")
+"""
+
+
+@gpu
+def test_a_failed_question_for_residency_is_an_error_and_is_asked_again():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FAILED_QUESTION], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "asked again" in r.stdout, r.stdout + r.stderr
