@@ -278,9 +278,11 @@ int moe_rmsnorm(const void* x, int T, int h, float eps, void* out, void* cuda_st
  * Residual addition with RMS norm, what a pre-norm block computes between two layers:
  *   s = x + residual, rounded to the tensors' type (the residual stream holds it),
  *   out = s * rstd * gain,  rstd = 1 / sqrt(mean(s^2) + eps),
- * everything between load and store in fp32; the norm is of s as it is held.
+ * everything between load and store in fp32, products from the left; the norm is of
+ * s as it is held.  A sum of squares beyond fp32 is infinite and rstd 0.
  *   x, residual, out, s [T][h], gain [h]  device, dtype (a moe_dtype); any h in
- *   1 .. 2^20.  residual NULL: s = x and the argument s is NULL too.  gain NULL: 1.
+ *   1 .. 2^20, but the tensors begin at multiples of 16 bytes (of an odd h not every
+ *   row does), rstd at one of 4.  residual NULL: s = x and the argument s is NULL too.  gain NULL: 1.
  *   rstd [T] fp32 device, or NULL: what the backward pass wants.
  * out and s may each be x or residual themselves (the same address); no other
  * overlap is allowed.  T = 0 is a no-op.  Asynchronous.
@@ -289,11 +291,13 @@ int moe_add_rmsnorm(const void* x, const void* residual, const void* gain, int T
                     int dtype, void* out, void* s, float* rstd, void* cuda_stream);
 
 /*
- * The same norm with an output in 8 bits: v = s * rstd * gain in fp32,
+ * The same norm with an output in 8 bits: v = (s * gain) * rstd in fp32, in this
+ * order (where s * gain leaves fp32's range, so does v: a scale of infinity with
+ * NaN and zeros, or 0),
  *   scale = max(max |v| / 448, 2^-126) over a row (group = 0) or over each 128
  *   columns of it (group = 128, h % 128 == 0),  q = e4m3(v / scale), to nearest even.
  *   q [T][h] e4m3 device (its value times its scale is v),
- *   scales [T] or [T][h / 128] fp32 device.
+ *   scales [T] or [T][h / 128] fp32 device, at a multiple of 4 bytes.
  * A NaN of v is a NaN of q and counts in no maximum.  q may not overlap an input.
  */
 int moe_add_rmsnorm_e4m3(const void* x, const void* residual, const void* gain, int T, int h,

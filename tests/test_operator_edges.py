@@ -176,3 +176,44 @@ def test_a_failed_question_for_residency_is_an_error_and_is_asked_again():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FAILED_QUESTION], cwd=root, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "asked again" in r.stdout, r.stdout + r.stderr
+
+
+@gpu
+@pytest.mark.parametrize("h", [256, 1024, 2048, 4096, 8320, 16384])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_e4m3_of_products_beyond_fp32(h, dt):
+    """s * gain overflows in the second group of 128 columns and underflows in the last: v = (s * gain) * rstd there is
+    infinite and 0, the other groups are as they would be alone."""
+    T = 5
+    g = torch.Generator(DEV).manual_seed(h)
+    s = (torch.randn((T, h), generator=g, device=DEV) * 1e15).to(dt)
+    s[:, 130] = 2e15
+    gain = (1 + 0.3 * torch.rand(h, generator=g, device=DEV)).to(dt)
+    plain_q, plain_scales, _ = binding.add_rmsnorm_e4m3(s, None, gain, group=128)
+    s[:, -128:] = (torch.randn((T, 128), generator=g, device=DEV) * 1e-20).to(dt)
+    gain[128:256], gain[-128:] = 1e25, 1e-30
+    if h == 256:  # the second group is the last
+        s[:, 130], gain[128:256] = 2e15, 1e25
+    p = s.float() * gain.float()  # infinite or 0 in fp32 too
+    q, scales, _ = binding.add_rmsnorm_e4m3(s, None, gain, group=128)
+    assert bool(p[:, 130].isinf().all()) and bool(scales[:, 1].isinf().all())
+    part, inf = q[:, 128:256].float(), p[:, 128:256].isinf()
+    assert bool(part[inf].isnan().all()) and not part[~inf].any()
+    if h > 256:
+        assert not p[:, -128:].any() and not q[:, -128:].float().any() and bool((scales[:, -1] == 2.0 ** -126).all())
+    # rstd of the whole row is another one now, but q and the ratio of two scales do not depend on it
+    keep = [i for i in range(h // 128) if i not in (1, h // 128 - 1)]
+    U = 2.0 ** -24
+    for i in keep:
+        a, b = (t[:, 128 * i:128 * (i + 1)].float() for t in (q, plain_q))
+        assert torch.equal(a, b)
+    if len(keep) > 1:
+        now, then = scales[:, keep].double(), plain_scales[:, keep].double()
+        ratio = (now / now[:, :1]) / (then / then[:, :1])
+        assert bool(((ratio - 1).abs() <= 16 * U).all())  # four scales of two roundings each, taken double
+    # a scale a row: infinite, NaN where the product is, 0 elsewhere
+    q, scales, _ = binding.add_rmsnorm_e4m3(s, None, gain)
+    assert bool(scales.isinf().all()) and bool(q.float()[p.isinf()].isnan().all()) and not q.float()[~p.isinf()].any()
+    # the norm in the tensors' type takes s * rstd first
+    out, _ = binding.add_rmsnorm(s, None, gain)
+    assert bool(out.isfinite().all())
