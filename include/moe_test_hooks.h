@@ -100,6 +100,9 @@ int moe_test_hold(unsigned ms, void* cuda_stream);
  */
 int moe_test_fail_occupancy(int times);
 
+/* 1 where launches may start before their predecessors end, 0 with MOE_NO_PDL=1. */
+int moe_test_early_launches(void);
+
 #ifdef __cplusplus
 }
 #endif

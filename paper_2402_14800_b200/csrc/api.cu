@@ -620,8 +620,7 @@ moe_layer_t* moe_layer_create(const void* W_gate, const void* W1, const void* W3
   L->decode_kernel = (dk && !strcmp(dk, "wm")) ? 1 : ((dk && !strcmp(dk, "td")) ? 2 : 0);
   const char* sk = getenv("MOE_SINGLE_KERNEL");
   L->single_gemv = !(sk && !strcmp(sk, "gemm")) && L->decode_kernel == 0 && gemv_single_fits(h, f);
-  const char* nopdl = getenv("MOE_NO_PDL");
-  if (nopdl) g_pdl_enabled = nopdl[0] != '1';
+  g_pdl_enabled = pdl_from_environment(g_pdl_enabled);
   const char* dense = getenv("MOE_SEARCH_DENSE");
   L->search_dense = dense && dense[0] == '1';
 
@@ -708,6 +707,8 @@ int moe_reserve(moe_layer_t* L, int T_max) {
   if ((rc = ensure_gemm(L, T_max))) return rc;
   return MOE_OK;
 }
+
+int moe_test_early_launches(void) { return g_pdl_enabled ? 1 : 0; }
 
 void moe_test_set_free_bytes_limit(long long bytes) { g_free_bytes_limit = bytes; }
 

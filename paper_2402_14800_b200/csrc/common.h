@@ -5,6 +5,9 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <stdlib.h>
+
+#include <atomic>
 
 #include "moe.h"
 
@@ -159,8 +162,13 @@ __device__ __forceinline__ void pdl_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// MOE_NO_PDL=1 (read when a handle is created) launches everything with plain stream order.
-inline bool g_pdl_enabled = true;
+// MOE_NO_PDL=1 launches everything with plain stream order.  Read when the library is loaded, for calls without a handle,
+// and again when a handle is created; one switch for the process.
+inline bool pdl_from_environment(bool otherwise) {
+  const char* v = getenv("MOE_NO_PDL");
+  return v ? v[0] != '1' : otherwise;
+}
+inline std::atomic<bool> g_pdl_enabled{pdl_from_environment(true)};
 
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,

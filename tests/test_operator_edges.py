@@ -104,6 +104,20 @@ def test_the_largest_sizes_have_plans(lib):
     assert r.returncode == 0 and "planned" in r.stdout, (r.returncode, r.stdout + r.stderr)
 
 
+@pytest.mark.parametrize("value,early", [(None, 1), ("0", 1), ("1", 0)])
+def test_plain_stream_order_is_read_for_calls_without_a_handle(lib, value, early):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = {k: v for k, v in os.environ.items() if k != "MOE_NO_PDL"}
+    if value is not None:
+        env["MOE_NO_PDL"] = value
+    code = "from paper_2402_14800_b200 import binding; print(binding.load_library().moe_test_early_launches())"
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, env=env, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == str(early), r.stdout + r.stderr
+
+
 # ------------------------------------------------------------------------------- on the device
 
 
