@@ -348,7 +348,8 @@ size_t moe_ffn_saved_bytes(int T, int f);
 size_t moe_ffn_forward_workspace(int T, int h, int f);
 
 /*
- * Gradients of moe_ffn_forward from dy and what the forward call saved:
+ * Gradients of moe_ffn_forward from dy and what the forward call saved (the routed
+ * layer has none: where its output was added to y, x gets no gradient through it):
  *   da = dy W2,  dg = da * u * silu'(g),  du = da * silu(g)
  *   dx = dg W1 + du W3,  dW1 = dg^T x,  dW3 = du^T x,  dW2 = dy^T a
  * (the residual's gradient is dy).  dy, dx [T][h], dW1, dW3 [f][h], dW2 [h][f]

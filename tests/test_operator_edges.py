@@ -231,3 +231,40 @@ def test_e4m3_of_products_beyond_fp32(h, dt):
     # the norm in the tensors' type takes s * rstd first
     out, _ = binding.add_rmsnorm(s, None, gain)
     assert bool(out.isfinite().all())
+
+
+@gpu
+@pytest.mark.parametrize("T", [3, 50, 300])
+def test_the_documented_backward_is_the_gradient_of_the_documented_forward(T):
+    """The README's lines from the forward calls to the gradients, run as they stand, against the 64-bit gradient of their y.
+
+    Tolerance, in the 2-norm: a rounding is off by at most half a step, 2^-8 of a value in bf16; behind an output stand no
+    more than eight (n, a, dg, du, dn, what they are multiplied with being given, and the output itself; p and q
+    are fp32), and products of random operands keep the relative size of independent errors."""
+    import os
+    import re
+
+    from paper_2402_14800_b200 import synth
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with open(os.path.join(root, "README.md")) as file:
+        blocks = re.findall(r"(?:^ {6}.*\n)+", file.read(), re.M)
+    code = [b for b in blocks if "binding.ffn_backward" in b]
+    assert len(code) == 1 and sum("binding.add_rmsnorm(" in b for b in blocks) == 2
+    h, f, E = synth.TINY["h"], synth.TINY["f"], synth.TINY["E"]
+    L = synth.make_layer_weights(h, f, E, seed=0)
+    layer = binding.MoeLayer(*[t.to(DEV) for t in (L.W_gate, L.W1, L.W3, L.W2)])
+    x, W1, W3, W2, dy = block_inputs(T, h, f, torch.bfloat16, seed=4)
+    residual = block_inputs(T, h, 8, torch.bfloat16, seed=5)[0]
+    gain = (1 + 0.1 * block_inputs(1, h, 8, torch.bfloat16, seed=6)[0][0].float()).bfloat16()
+    names = dict(torch=torch, binding=binding, layer=layer, beta=0.0, T=T, f=f, device=DEV, x=x, residual=residual, gain=gain,
+                 W1=W1, W3=W3, W2=W2, dy=dy)
+    exec("\n".join(line[6:] for line in code[0].splitlines()), names)
+    s, gn, w1, w3, w2 = leaves = [t.double().requires_grad_() for t in (names["s"], gain, W1, W3, W2)]
+    n = s * torch.rsqrt(s.square().mean(1, keepdim=True) + 1e-5) * gn
+    g = n @ w1.T
+    y = (g * torch.sigmoid(g) * (n @ w3.T)) @ w2.T + s
+    y.backward(dy.double())
+    for k, want in [("y", y.detach()), *zip(("dx", "dgain", "dW1", "dW3", "dW2"), (t.grad for t in leaves))]:
+        off = float((names[k].double() - want).norm() / want.norm())
+        assert off < 8 * 2.0 ** -8, (k, off)
+    layer.close()
