@@ -268,3 +268,41 @@ def test_the_documented_backward_is_the_gradient_of_the_documented_forward(T):
         off = float((names[k].double() - want).norm() / want.norm())
         assert off < 8 * 2.0 ** -8, (k, off)
     layer.close()
+
+
+@gpu
+def test_sums_over_tokens_beyond_32_bit_offsets():
+    """The weights' gradients where a, dg, du and the saved values pass 2^31 elements: with dy zero but for the last tokens
+    they are those tokens' alone, and a range that is dropped, doubled or read elsewhere would show."""
+    from tests.test_ffn_ops import check, reference
+    T, h, f = 150100, 64, 14336
+    assert T * f > 2 ** 31
+    x, W1, W3, W2, dy = block_inputs(T, h, f, torch.bfloat16, seed=9)
+    last = slice(T - 100, T)
+    dy[:T - 100] = 0
+    saved = binding.ffn_saved(T, f, DEV)
+    binding.ffn_forward(x, W1, W3, W2, saved=saved)
+    _, *grads = binding.ffn_backward(dy, x, W1, W3, W2, saved)
+    want = reference(x[last].clone(), W1, W3, W2, dy[last].clone())
+    for k, v in zip(("dW1", "dW3", "dW2"), grads):
+        check(v, want[k], torch.bfloat16, k)
+
+
+@gpu
+def test_gradient_of_the_gain_beyond_32_bit_offsets():
+    # rows of zeros add nothing, whatever their d_out: the sum is that of the last three rows
+    T, h = 33000, 65544
+    assert T * h > 2 ** 31
+    g = torch.Generator(DEV).manual_seed(4)
+    s = torch.zeros((T, h), dtype=torch.bfloat16, device=DEV)
+    s[-3:] = torch.randn((3, h), generator=g, device=DEV)
+    d_out = torch.ones((T, h), dtype=torch.bfloat16, device=DEV)
+    d_out[-3:] = torch.randn((3, h), generator=g, device=DEV)
+    gain = torch.ones(h, dtype=torch.bfloat16, device=DEV)
+    rstd = torch.rsqrt(s.new_zeros(T, dtype=torch.float32) + 1e-5)
+    rstd[-3:] = torch.rsqrt(s[-3:].double().square().mean(1) + 1e-5).float()
+    _, dgain = binding.add_rmsnorm_backward(d_out, s, rstd, gain)
+    terms = d_out[-3:].double() * s[-3:].double() * rstd[-3:].double()[:, None]
+    # a term is two roundings of 2^-24, the sum of three in any order two more; dgain one of 2^-8
+    tol = 2.0 ** -8 * 1.01 * terms.sum(0).abs() + 4 * 2.0 ** -24 * terms.abs().sum(0) + torch.finfo(torch.bfloat16).smallest_normal
+    assert bool(((dgain.double() - terms.sum(0)).abs() <= tol).all())
