@@ -365,7 +365,8 @@ def rmsnorm(x, eps: float = 1e-5, out=None, stream=None):
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # a tenth of the time of torch.cuda.current_stream().cuda_stream
+# a tenth of the time of torch.cuda.current_stream().cuda_stream, but a private name that not every torch has
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _operand(name, t, dtype, shape, index):

@@ -118,6 +118,29 @@ def test_plain_stream_order_is_read_for_calls_without_a_handle(lib, value, early
     assert r.returncode == 0 and r.stdout.strip() == str(early), r.stdout + r.stderr
 
 
+WITHOUT_CUDA = """
+import torch
+assert hasattr(torch._C, "_cuda_getCurrentRawStream")
+del torch._C._cuda_getCurrentRawStream  # as in a torch built without CUDA
+import paper_2402_14800_b200
+from paper_2402_14800_b200 import binding
+assert binding.load_library().moe_num_subsets(8, 6) == 28
+try:
+    binding.add_rmsnorm(torch.zeros(4, 64))
+except binding.MoeError:
+    print("refused")
+"""
+
+
+def test_binding_loads_where_torch_has_no_cuda(lib):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", WITHOUT_CUDA], cwd=root, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "refused" in r.stdout, r.stdout + r.stderr
+
+
 # ------------------------------------------------------------------------------- on the device
 
 
