@@ -336,9 +336,11 @@ size_t moe_add_rmsnorm_backward_workspace(int T, int h);
  *   workspace: device memory of moe_ffn_forward_workspace(T, h, f) bytes for the
  *   current device, free again when the call's kernels are done; calls that may
  *   run at the same time need one each.
- * a is rounded to the tensors' type, y once; everything else is fp32.  Both
- * projections, the activation and the product are one launch.  The weights are
- * read where they are: nothing is kept between calls.  T = 0 is a no-op.
+ * a is rounded to the tensors' type (in fp16 an a beyond 65504 is infinite), y once;
+ * everything else is fp32.  Both projections, the activation and the product are one
+ * launch.  The same call gives the same bits; up to 32 tokens a call with saved runs
+ * other kernels than one without, whose y may differ in its last bits.  The weights
+ * are read where they are: nothing is kept between calls.  T = 0 is a no-op.
  * Asynchronous, and free of host synchronisation and allocation.
  */
 int moe_ffn_forward(const void* x, const void* W1, const void* W3, const void* W2,
@@ -353,7 +355,8 @@ size_t moe_ffn_forward_workspace(int T, int h, int f);
  *   da = dy W2,  dg = da * u * silu'(g),  du = da * silu(g)
  *   dx = dg W1 + du W3,  dW1 = dg^T x,  dW3 = du^T x,  dW2 = dy^T a
  * (the residual's gradient is dy).  dy, dx [T][h], dW1, dW3 [f][h], dW2 [h][f]
- * device, dtype; a, dg and du are rounded to dtype, each gradient once.  No
+ * device, dtype; a, dg and du are rounded to dtype (its range is theirs: a scaled
+ * loss is the caller's), each gradient once.  No
  * gradient may overlap an input or another gradient.  workspace as above, of
  * moe_ffn_backward_workspace(T, h, f) bytes.  Sums have a fixed order: the same
  * call gives the same bits.  T = 0 clears the weights' gradients.  Asynchronous.

@@ -360,7 +360,9 @@ def rmsnorm(x, eps: float = 1e-5, out=None, stream=None):
     return out
 
 
-# Operators on the caller's own tensors: no handle, scratch from torch's allocator on the call's stream.
+# Operators on the caller's own tensors: no handle, scratch from torch's allocator on the call's stream.  They read and
+# write memory and leave no autograd graph: what requires a gradient gets none through them, the backward passes
+# are calls of their own.
 
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 

@@ -51,8 +51,8 @@ enum Kind { kGateUp, kGateUpSave, kPlain, kDact, kGrads };
 // and the next launch's CTAs set up and fetch their first weights beside the last ones of this launch.  Forward pass in
 // us, full form / slim form, tokens 64 and 128: (h 512, f 1024) 18.6 / 16.3, 18.1 / 16.8; (2048, 4096) 31.7 / 29.8, 32.9 /
 // 33.9; (4096, 4096) 48.8 / 46.5, 50.6 / 63.9; (4096, 14336) 76.6 / 75.8, 78.9 / 90.9.  Up to 32 columns a matrix of 96 MB and
-// more streams longer than the gap costs, and the full form has more of it in flight: 8 tokens of (4096, 14336) 67.2 /
-// 69.9, of (4096, 8192) 50.0 / 49.7.
+// more streams longer than the gap costs, and the full form has more of it in flight: 8 tokens of (4096, 14336), 117 MB,
+// 67.2 / 69.9, of (4096, 8192), 67 MB, 50.0 / 49.7; where between the two the line lies was not measured.
 template <bool SLIM> struct Form {
   static constexpr int kEpiWarps = SLIM ? 4 : 16;
   static constexpr int kThreads = 96 + 32 * kEpiWarps;
@@ -683,7 +683,9 @@ Ring ring_of(int kind, int R, int n_tile, bool slim) {
 
 // Tile and split of a launch of M x N outputs and KB k-blocks, by a model in SM cycles.  A k-block of an item takes
 // the largest of
-//   4.6 n_tile          the tensor pipe: eight MMAs of n_tile / 2 cycles, which the ring of stages keeps 88 % busy,
+//   4.6 n_tile          the tensor pipe: eight MMAs of n_tile / 2 cycles, which the ring of stages keeps 88 % busy (an MMA of
+//                       M = 256 takes about 90 cycles at least, 720 a k-block, which the model knows of the weights'
+//                       gradients only: items of few columns and of fewer than 128 rows are reckoned too short),
 //   bytes / 7600        what all running pairs draw from L2, 128 bytes for each row of A and column of B
 //   bytes / 3800        what they draw from HBM: rows of A that no other running item shares,
 //   bytes / 110         what a pair by itself can draw,

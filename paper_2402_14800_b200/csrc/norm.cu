@@ -525,9 +525,12 @@ __global__ void __launch_bounds__(1024) dgain_reduce_kernel(const float* partial
 }
 
 // How a row is cut: threads a row and vectors a thread.  In the forward pass rows that 128 threads of two vectors fill to
-// three quarters and more take those: more rows are under way on an SM, and what a row waits for is its reduction.  Against
-// 256 threads of one vector (us): e4m3 of 8000 x 2048 fp16 20.5 -> 18.8, norm of 8192 x 2048 bf16 the same, but 30000 x
-// 1536 57.0 -> 61.  Three vectors a thread were 4-10 % slower than the next cut (1536 to 6144 columns).
+// three quarters and more take those: more rows are under way on an SM, and what a row waits for is its reduction.  256
+// threads of one vector / 128 of two, us, columns 1544 / 1792 / 2048 of bf16: e4m3 of 8000 rows 22.7 / 19.6, 22.9 / 19.9,
+// 24.0 / 20.9, of 30000 rows 76.7 / 65.9, 76.6 / 65.3, 79.5 / 68.5; norm of 8000 rows 18.1 / 17.9, 20.1 / 20.1, 22.6 / 22.8,
+// of 30000 rows 59.8 / 59.4, 72.9 / 74.5, 85.5 / 83.6.  fp32 of 772 to 1024 columns: e4m3 of 8000 rows 2-11 % faster, of
+// 30000 x 1024 61.1 / 64.3, norm within 2 %.  Single elements, 30000 x 193 to 255: norm 30 / 21, e4m3 48 / 33.  Below, 30000 x
+// 1536, it is slower: 57.0 / 61.  Three vectors a thread were 4-10 % slower than the next cut (1536 to 6144 columns).
 struct Cut { int tpr, nv; };
 Cut cut_of(int h, int E, bool forward) {
   const int n = h / E;
